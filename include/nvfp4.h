@@ -421,6 +421,104 @@ nvfp4_status nvfp4_quant_noise(const void *x, nvfp4_dtype dt, int64_t rows, int6
                                void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * ---- 8-bit linear layers and mixtures of experts
+ *
+ * Beside the FP4 layers a model keeps some in 8 bits (those that do not bear 4, and all of them in a closing phase
+ * of training at more bits), and its MLP may be a mixture of experts: each token goes to top_k of E weight
+ * matrices.  The calls below are such a layer's parts; the paper has none of them.
+ *
+ * An 8-bit operand of a logical [rows, K] tensor: with S = ceil(K / 128) blocks of 128 along the contraction,
+ *   codes   [rows, 128 S] bytes, E4M3 (bias 7, finite-only, 0x7F / 0xFF are NaN), zero past K;
+ *   scales  [S, rows] bytes, E8M0 (2^(byte - 127)): block-major, the bytes of neighbouring rows side by side.
+ * Pointers and pitches of tensors (x, out, y, ...) need the alignment of an element only; codes must be 16-byte aligned.
+ * Empty tensors (a size of 0) are accepted where said; their pointers may be NULL.
+ */
+size_t nvfp4_fp8_codes_bytes(int64_t rows, int64_t K);
+size_t nvfp4_fp8_scales_bytes(int64_t rows, int64_t K);
+
+/*
+ * Quantization to such operands.  Per block: a = max|x|, e = the smallest exponent with a <= 448 * 2^e, at least
+ * -127; byte = e + 127; code = E4M3(x * 2^-e), nearest, ties to even: nothing else rounds.  A zero block has byte 0.  A block that
+ * holds an infinity or a NaN becomes NaN codes with byte 127, so that the product shows it.
+ *   x       `batch` matrices [rows, cols] of dt, one behind the other, all with row pitch ld (elements)
+ *   rows side (codes_rows, scales_rows; both NULL: not wanted): blocks along the columns, an operand of batch * rows
+ *           rows with K = cols;
+ *   columns side (codes_cols, scales_cols; both NULL: not wanted): blocks down each matrix' columns, an operand of
+ *           batch * cols rows with K = rows: the quantized transposes.
+ * Both sides together read x once.
+ *   order   NULL, or device int32 [rows] (batch 1): row r of the matrix is row order[r] / top_k of x, which has x_rows
+ *           rows; zeros where that is negative or past x_rows (nvfp4_moe_sort writes it; gathering costs no pass)
+ *   offsets NULL, or device int32 [groups + 1] (batch 1, columns side wanted), ascending from 0 to at most rows: the rows
+ *           offsets[e] .. offsets[e + 1] - 1 are group e's, and the column blocks start anew at its first row.  The columns
+ *           operand then has S = nvfp4_fp8_slots(rows, groups) blocks, of which group e's are those from
+ *           offsets[e] / 128 + e on, ceil(its rows / 128) of them, its last one filled up with zeros; blocks of no group, and the
+ *           row side of rows of no group, are neither written here nor read by the products.  groups: 1 .. 512.
+ * batch, rows or cols of 0: nothing is written.
+ */
+int64_t nvfp4_fp8_slots(int64_t rows, int64_t groups);
+nvfp4_status nvfp4_fp8_quantize(const void *x, nvfp4_dtype dt, int64_t batch, int64_t rows, int64_t cols, int64_t ld,
+                                const int32_t *order, int32_t top_k, int64_t x_rows, const int32_t *offsets, int32_t groups,
+                                uint8_t *codes_rows, uint8_t *scales_rows, uint8_t *codes_cols, uint8_t *scales_cols,
+                                void *stream);
+
+/*
+ * out[i, j] = sum_k a[i, k] b[j, k] of two operands [M, K] and [N, K], K a multiple of 128 (the operands' padded
+ * width).  out: [M, N] of out_dt with row pitch ldc.  Products and scales are exact, sums are binary32, rounded
+ * once to out_dt; their order follows from the sizes and the same call gives the same bits.  M or N of 0: nothing; K of 0: zeros.
+ */
+nvfp4_status nvfp4_fp8_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *A_codes, const uint8_t *A_scales,
+                            const uint8_t *B_codes, const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc,
+                            void *stream);
+/*
+ * The experts' products.  A [rows, K] holds the gathered tokens in the experts' order, offsets (device int32
+ * [groups + 1], ascending, 0 .. rows) says which are whose, B is an operand of groups * N rows, expert e's N from e N on:
+ *   out[r, :] = A[r, :] B_e^T     for offsets[e] <= r < offsets[e + 1]; zeros for rows of no expert.
+ * The backward product is the same call on the gradient and the transposed weights' operand.
+ */
+nvfp4_status nvfp4_fp8_gemm_experts(int64_t rows, int64_t N, int64_t K, int32_t groups, const int32_t *offsets,
+                                    const uint8_t *A_codes, const uint8_t *A_scales, const uint8_t *B_codes,
+                                    const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc, void *stream);
+/*
+ * The experts' weight gradients: A [M, 128 S] and B [N, 128 S] are columns operands of two tensors of `rows` rows with these
+ * offsets, S = nvfp4_fp8_slots(rows, groups);
+ *   out[e] = sum over the rows r of expert e of a[r, :]^T b[r, :],     out [groups, M, N] of out_dt, row pitch ldc
+ * (zeros for an expert without rows).
+ */
+nvfp4_status nvfp4_fp8_gemm_experts_dw(int64_t M, int64_t N, int64_t rows, int32_t groups, const int32_t *offsets,
+                                       const uint8_t *A_codes, const uint8_t *A_scales, const uint8_t *B_codes,
+                                       const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc, void *stream);
+
+/*
+ * (token, choice) pairs sorted by expert.  experts: device [pairs] of integers of id_bytes (4 or 8) bytes, pair = token *
+ * top_k + choice; a number outside 0 .. groups - 1 drops its pair.
+ *   offsets  [groups + 1]: expert e's pairs take the slots offsets[e] .. offsets[e + 1] - 1, in the pairs' order;
+ *   order    [pairs]: the pair in each slot, -1 past the last;   position [pairs]: the slot of each pair, -1 if dropped.
+ * groups 1 .. 512, pairs up to 2^31 - 1 (0: offsets alone).  workspace: >= nvfp4_moe_sort_workspace_bytes(pairs, groups) bytes,
+ * 4-byte aligned, NULL where that is 0.
+ */
+size_t nvfp4_moe_sort_workspace_bytes(int64_t pairs, int32_t groups);
+nvfp4_status nvfp4_moe_sort(const void *experts, int32_t id_bytes, int64_t pairs, int32_t groups, int32_t *offsets,
+                            int32_t *order, int32_t *position, void *workspace, size_t workspace_bytes, void *stream);
+/* out[r] = x[order[r] / top_k] of x [x_rows, cols] (pitch ld), zeros where that names no row; out [rows, cols] dense. */
+nvfp4_status nvfp4_moe_gather(const void *x, nvfp4_dtype dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order,
+                              int32_t top_k, int64_t rows, void *out, void *stream);
+/*
+ * out[t] = sum_j weights[t, j] y[position[t, j]] over the choices that were not dropped, in their order, in binary32;
+ * y [rows, cols], out [tokens, cols] dense, of dt.  weights: device fp32 [tokens, top_k], or NULL for ones (the
+ * gradient of nvfp4_moe_gather).  A token without a choice gets zeros.
+ */
+nvfp4_status nvfp4_moe_combine(const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols, const float *weights,
+                               const int32_t *position, int64_t tokens, int32_t top_k, void *out, void *stream);
+/*
+ * Its gradient for the upstream dout [tokens, cols]: dy[position[t, j]] = weights[t, j] dout[t] and dweights[t, j] =
+ * dout[t] . y[position[t, j]] (binary32; 0 for a dropped pair).  offsets: of the sort, [groups + 1]; rows of dy past
+ * the last kept pair are set to zero.  dy must not share memory with y.
+ */
+nvfp4_status nvfp4_moe_combine_bwd(const void *dout, const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols,
+                                   const float *weights, const int32_t *position, const int32_t *offsets, int32_t groups,
+                                   int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream);
+
+/*
  * Diagnostic, not part of the method: the sustained rate of the matrix
  * instruction a GEMM kernel issues, measured on the current device from a
  * register-only loop (no LDS or global traffic) in that kernel's register-tile

@@ -1,0 +1,377 @@
+// Routing of tokens to experts: (token, choice) pairs sorted by expert, rows moved between the tokens' order and the experts', and the gradients
+// of that.  pair = token * top_k + choice.
+//   sort          a stable counting sort: every pair's slot is the number of pairs of smaller experts plus that of earlier pairs of its own.
+//                 No atomic decides an order, so the answer is the same from call to call.
+//   gather        out[slot] = x[order[slot] / top_k]
+//   combine       out[t] = sum_j w[t, j] y[position[t, j]], choices in their order, binary32
+//   combine_bwd   dy[position[t, j]] = w[t, j] dout[t],  dw[t, j] = sum_d dout[t, d] y[position[t, j], d]
+// All of it is bound by memory; a wave moves a row (of a pair, or of a token with its choices) in pieces of 16 bytes a lane.
+#include "experts.h"
+
+namespace nvfp4 {
+namespace moe {
+
+constexpr int WAVES = 16, NT = 64 * WAVES;
+
+// Exclusive prefix sum of one value per thread over the workgroup; *total receives the sum
+__device__ __forceinline__ int prefix(int v, int *per_wave, int *total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(s, d);
+        if (lane >= d) s += up;
+    }
+    if (lane == 63) per_wave[wave] = s;
+    __syncthreads();
+    int before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const int n = per_wave[w];
+        if (w < wave) before += n;
+        sum += n;
+    }
+    __syncthreads();
+    *total = sum;
+    return before + s - v;
+}
+
+template <typename ID>
+__device__ __forceinline__ int expert_of(const ID *ids, int64_t i, int64_t n, int groups)
+{
+    if (i >= n) return -1;
+    const ID e = ids[i];
+    return e >= 0 && e < (ID)groups ? (int)e : -1;
+}
+
+}  // namespace moe
+
+// Pairs of each expert in each workgroup's part of them: counts [workgroups, groups]
+template <typename ID>
+__global__ __launch_bounds__(1024) void moe_count_kernel(const ID *ids, int64_t n, int groups, int64_t part, int32_t *counts)
+{
+    using namespace moe;
+    extern __shared__ int hist[];
+    for (int e = threadIdx.x; e < groups; e += NT) hist[e] = 0;
+    __syncthreads();
+    const int64_t first = blockIdx.x * part, last = first + part < n ? first + part : n;
+    for (int64_t i = first + threadIdx.x; i < last; i += NT) {
+        const int e = expert_of(ids, i, last, groups);
+        if (e >= 0) atomicAdd(&hist[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < groups; e += NT) counts[(int64_t)blockIdx.x * groups + e] = hist[e];
+}
+
+// A workgroup places its part of the pairs.  Its waves take consecutive pieces of the part; a wave places 64 pairs at a time, a lane's rank
+// among those of its expert from one ballot per bit of the expert's number.  counts: of all parts, null for one part.
+template <typename ID>
+__global__ __launch_bounds__(1024) void moe_place_kernel(const ID *ids, int64_t n, int groups, int64_t part, const int32_t *counts, int32_t *offsets,
+                                                         int32_t *order, int32_t *position)
+{
+    using namespace moe;
+    extern __shared__ int hist[];  // [WAVES][groups], first counts and then the next free slot
+    __shared__ int per_wave[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = blockIdx.x * part, last = first + part < n ? first + part : n;
+    const int64_t piece = (part / WAVES + 63) / 64 * 64, w0 = first + wave * piece, w1 = w0 + piece < last ? w0 + piece : last;
+    int *const mine = hist + wave * groups;
+    for (int i = tid; i < WAVES * groups; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int64_t i = w0 + lane; i < w1; i += 64) {
+        const int e = expert_of(ids, i, w1, groups);
+        if (e >= 0) atomicAdd(&mine[e], 1);
+    }
+    __syncthreads();
+    // thread e: the expert's pairs of all parts, of the parts before this one, of the waves before each (groups <= NT)
+    int all = 0, before = 0;
+    if (tid < groups) {
+        if (counts) {
+            for (unsigned b = 0; b < gridDim.x; ++b) {
+                const int k = counts[(int64_t)b * groups + tid];
+                all += k;
+                if (b < blockIdx.x) before += k;
+            }
+        } else {
+            for (int w = 0; w < WAVES; ++w) all += hist[w * groups + tid];
+        }
+    }
+    int total;
+    const int start = prefix(all, per_wave, &total);
+    if (tid < groups) {
+        int at = start + before;
+        for (int w = 0; w < WAVES; ++w) {
+            const int k = hist[w * groups + tid];
+            hist[w * groups + tid] = at;
+            at += k;
+        }
+        if (blockIdx.x == 0) offsets[tid] = start;
+    }
+    if (blockIdx.x == 0 && tid == 0) offsets[groups] = total;
+    __syncthreads();
+    const int bits = 32 - __builtin_clz((unsigned)groups);
+    for (int64_t i0 = w0; i0 < w1; i0 += 64) {
+        const int64_t i = i0 + lane;
+        const int e = expert_of(ids, i, w1, groups);
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 0; b < bits; ++b) {
+            const uint64_t ones = __ballot((e >> b) & 1);
+            same &= (e >> b) & 1 ? ones : ~ones;
+        }
+        if (e >= 0) {
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int slot = *const_cast<volatile int *>(&mine[e]) + rank;
+            if (rank == 0) atomicAdd(&mine[e], __popcll(same));  // (behind the wave's reads: LDS accesses of a wave keep their order)
+            order[slot] = (int32_t)i;
+            position[i] = slot;
+        } else if (i < w1) {
+            position[i] = -1;
+        }
+    }
+    for (int64_t i = first + tid; i < last; i += NT)
+        if (i >= total) order[i] = -1;
+}
+
+namespace moe {
+constexpr int64_t PART = 4096;       // pairs of a workgroup
+constexpr int64_t MOST_PARTS = 256;  // (every workgroup reads the counts of all)
+inline int64_t part_of(int64_t n)
+{
+    int64_t part = n <= 2 * PART ? (n > 0 ? n : 1) : PART;
+    if ((n + part - 1) / part > MOST_PARTS) part = (n + MOST_PARTS - 1) / MOST_PARTS;
+    return (part + NT - 1) / NT * NT;
+}
+}  // namespace moe
+
+size_t moe_sort_workspace(int64_t pairs, int32_t groups)
+{
+    const int64_t part = moe::part_of(pairs), parts = (pairs + part - 1) / part;
+    return parts > 1 ? (size_t)parts * groups * 4 : 0;
+}
+
+template <typename ID>
+static hipError_t sort(const ID *ids, int64_t n, int32_t groups, int32_t *offsets, int32_t *order, int32_t *position, int32_t *counts, hipStream_t st)
+{
+    using namespace moe;
+    const int64_t part = part_of(n), parts = n > 0 ? (n + part - 1) / part : 1;
+    if (parts > 1) moe_count_kernel<ID><<<dim3((unsigned)parts), NT, groups * 4, st>>>(ids, n, groups, part, counts);
+    moe_place_kernel<ID><<<dim3((unsigned)parts), NT, WAVES * groups * 4, st>>>(ids, n, groups, part, parts > 1 ? counts : nullptr, offsets, order, position);
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_sort(const void *experts, int id_bytes, int64_t pairs, int32_t groups, int32_t *offsets, int32_t *order, int32_t *position,
+                           int32_t *workspace, hipStream_t st)
+{
+    return id_bytes == 8 ? sort(reinterpret_cast<const int64_t *>(experts), pairs, groups, offsets, order, position, workspace, st)
+                         : sort(reinterpret_cast<const int32_t *>(experts), pairs, groups, offsets, order, position, workspace, st);
+}
+
+namespace moe {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float float2v_t __attribute__((ext_vector_type(2)));
+
+// 16 bytes of a row at any element
+template <int DT>
+struct Piece {
+    static constexpr int N = DT == NVFP4_BF16 ? 8 : 4, ESZ = DT == NVFP4_BF16 ? 2 : 4;
+    struct __attribute__((packed, aligned(2))) P2 { u32x4_t w; };
+    struct __attribute__((packed, aligned(4))) P4 { u32x4_t w; };
+    u32x4_t w;
+    __device__ __forceinline__ void load(const uint8_t *p)
+    {
+        w = DT == NVFP4_BF16 ? reinterpret_cast<const P2 *>(p)->w : reinterpret_cast<const P4 *>(p)->w;
+    }
+    __device__ __forceinline__ void store(uint8_t *p) const
+    {
+        if (DT == NVFP4_BF16) reinterpret_cast<P2 *>(p)->w = w;
+        else reinterpret_cast<P4 *>(p)->w = w;
+    }
+    __device__ __forceinline__ void load_some(const uint8_t *p, int n)
+    {
+        w = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) {
+                if (DT == NVFP4_BF16) w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i & 1));
+                else w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+            }
+    }
+    __device__ __forceinline__ void store_some(uint8_t *p, int n) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) {
+                if (DT == NVFP4_BF16) reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+                else reinterpret_cast<uint32_t *>(p)[i] = w[i];
+            }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        return DT == NVFP4_BF16 ? __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) : __uint_as_float(w[i & 3]);
+    }
+    __device__ __forceinline__ void set(const float (&v)[N])
+    {
+        if (DT == NVFP4_BF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2v_t f = {v[(2 * i) % N], v[(2 * i + 1) % N]};
+                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+        }
+    }
+};
+
+// Calls body(offset in bytes, elements there) for a lane's pieces of a row: whole pieces first, U of them side by side
+template <int DT, class F>
+__device__ __forceinline__ void pieces(int64_t cols, int lane, F &&body)
+{
+    constexpr int N = Piece<DT>::N;
+    for (int64_t i = (int64_t)lane * N; i < cols; i += 64 * N) body(i * Piece<DT>::ESZ, (int)(cols - i < N ? cols - i : N));
+}
+
+}  // namespace moe
+
+template <int DT>
+__global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k,
+                                                         int64_t rows, uint8_t *out)
+{
+    using namespace moe;
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (r >= rows) return;
+    const int32_t pair = order[r];
+    const int64_t src = pair < 0 || pair / top_k >= x_rows ? -1 : pair / top_k;
+    const uint8_t *const from = x + src * ld * Piece<DT>::ESZ;
+    uint8_t *const to = out + r * cols * Piece<DT>::ESZ;
+    pieces<DT>(cols, lane, [&](int64_t at, int n) {
+        Piece<DT> v;
+        v.w = u32x4_t{0, 0, 0, 0};
+        if (n == Piece<DT>::N) {
+            if (src >= 0) v.load(from + at);
+            v.store(to + at);
+        } else {
+            if (src >= 0) v.load_some(from + at, n);
+            v.store_some(to + at, n);
+        }
+    });
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position,
+                                                          int64_t tokens, int32_t top_k, uint8_t *out)
+{
+    using namespace moe;
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= tokens) return;
+    pieces<DT>(cols, lane, [&](int64_t at, int n) {
+        float sum[Piece<DT>::N];
+#pragma unroll
+        for (int i = 0; i < Piece<DT>::N; ++i) sum[i] = 0.0f;
+        for (int j = 0; j < top_k; ++j) {
+            const int32_t p = position[t * top_k + j];
+            if (p < 0 || p >= y_rows) continue;
+            const float w = weights ? weights[t * top_k + j] : 1.0f;
+            Piece<DT> v;
+            const uint8_t *const from = y + ((int64_t)p * cols) * Piece<DT>::ESZ + at;
+            if (n == Piece<DT>::N) v.load(from);
+            else v.load_some(from, n);
+#pragma unroll
+            for (int i = 0; i < Piece<DT>::N; ++i) sum[i] = __builtin_fmaf(w, v.get(i), sum[i]);
+        }
+        Piece<DT> v;
+        v.set(sum);
+        if (n == Piece<DT>::N) v.store(out + t * cols * Piece<DT>::ESZ + at);
+        else v.store_some(out + t * cols * Piece<DT>::ESZ + at, n);
+    });
+}
+
+// A wave for each pair; behind them the waves that clear the rows of dy past the last kept pair
+template <int DT>
+__global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dout, const uint8_t *y, int64_t rows, int64_t cols, const float *weights,
+                                                              const int32_t *position, const int32_t *kept, int64_t pairs, int32_t top_k, uint8_t *dy,
+                                                              float *dweights)
+{
+    using namespace moe;
+    constexpr int N = Piece<DT>::N;
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = cols * Piece<DT>::ESZ;
+    if (id >= pairs) {
+        const int64_t clearing = (int64_t)gridDim.x * 4 - pairs;
+        for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
+            pieces<DT>(cols, lane, [&](int64_t at, int n) {
+                Piece<DT> v;
+                v.w = u32x4_t{0, 0, 0, 0};
+                if (n == N) v.store(dy + r * row + at);
+                else v.store_some(dy + r * row + at, n);
+            });
+        return;
+    }
+    const int32_t p = position[id];
+    if (p < 0 || p >= rows) {
+        if (lane == 0) dweights[id] = 0.0f;
+        return;
+    }
+    const uint8_t *const up = dout + id / top_k * row, *const from = y + p * row;
+    uint8_t *const to = dy + p * row;
+    const float w = weights[id];
+    float dot = 0.0f;
+    pieces<DT>(cols, lane, [&](int64_t at, int n) {
+        Piece<DT> a, b;
+        if (n == N) {
+            a.load(up + at);
+            b.load(from + at);
+        } else {
+            a.load_some(up + at, n);
+            b.load_some(from + at, n);
+        }
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = w * a.get(i);
+            dot = __builtin_fmaf(a.get(i), b.get(i), dot);
+        }
+        a.set(v);
+        if (n == N) a.store(to + at);
+        else a.store_some(to + at, n);
+    });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+    if (lane == 0) dweights[id] = dot;
+}
+
+hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out,
+                             hipStream_t st)
+{
+    auto *k = dt == NVFP4_BF16 ? moe_gather_kernel<NVFP4_BF16> : moe_gather_kernel<NVFP4_F32>;
+    k<<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
+                                                       reinterpret_cast<uint8_t *>(out));
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_combine(const void *y, int dt, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position, int64_t tokens,
+                              int32_t top_k, void *out, hipStream_t st)
+{
+    auto *k = dt == NVFP4_BF16 ? moe_combine_kernel<NVFP4_BF16> : moe_combine_kernel<NVFP4_F32>;
+    k<<<dim3((unsigned)((tokens + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position, tokens, top_k,
+                                                         reinterpret_cast<uint8_t *>(out));
+    return hipGetLastError();
+}
+
+hipError_t launch_moe_combine_bwd(const void *dout, const void *y, int dt, int64_t rows, int64_t cols, const float *weights, const int32_t *position,
+                                  const int32_t *kept, int64_t tokens, int32_t top_k, void *dy, float *dweights, hipStream_t st)
+{
+    const int64_t pairs = tokens * top_k, clearing = rows < 256 ? rows : 256;
+    auto *k = dt == NVFP4_BF16 ? moe_combine_bwd_kernel<NVFP4_BF16> : moe_combine_bwd_kernel<NVFP4_F32>;
+    k<<<dim3((unsigned)((pairs + clearing + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols,
+                                                                   weights, position, kept, pairs, top_k, reinterpret_cast<uint8_t *>(dy), dweights);
+    return hipGetLastError();
+}
+
+}  // namespace nvfp4
