@@ -71,6 +71,8 @@ struct Fp8GemmArgs {
     const int32_t *offsets;
     int32_t groups, total;                // total (FP8_EXPERTS_DW): the rows that the offsets divide
 };
+bool fp8_gemm_is_thin(const Fp8GemmArgs &P, int mode);  // few rows: of all, or of each expert on average
+hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 
 // Routing

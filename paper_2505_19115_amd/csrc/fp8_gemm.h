@@ -1,0 +1,211 @@
+// What the kernels of 8-bit products share: which rows and K tiles a workgroup's tile covers, scale bytes, fragments, and the way out.
+#pragma once
+#include "experts.h"
+
+namespace nvfp4 {
+namespace f8g {
+
+typedef int int8v_t __attribute__((ext_vector_type(8)));
+typedef float float4v_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float float2v_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int KT = FP8_BLOCK;
+
+// What a workgroup multiplies: rows m0 .. m0 + rows - 1 of A (and of the output that starts at out) against rows n0 .. n0 + cols - 1 of B,
+// K tiles k0 .. k0 + count - 1; b0 + column is a row of B.  rows <= 0: nothing.
+struct Tile {
+    int64_t m0, n0, b0, out;
+    int rows, cols, k0, count;
+};
+
+// Tiles of a launch
+template <int MODE>
+inline int64_t tiles(const Fp8GemmArgs &P, int BM, int BN)
+{
+    const int64_t ntx = (P.N + BN - 1) / BN, nty = (P.M + BM - 1) / BM;
+    return ntx * (MODE == FP8_EXPERTS ? P.M / BM + P.groups + 1 : MODE == FP8_EXPERTS_DW ? nty * P.groups : nty);
+}
+
+template <int MODE>
+__device__ __forceinline__ Tile find_tile(const Fp8GemmArgs &P, unsigned id, int BM, int BN)
+{
+    Tile T;
+    const int ntx = (int)((P.N + BN - 1) / BN);
+    T.k0 = 0;
+    T.count = P.blocks;
+    T.b0 = 0;
+    T.out = 0;
+    int ty = (int)(id / (unsigned)ntx), tx = (int)(id % (unsigned)ntx);
+    int64_t left;
+    if (MODE == FP8_EXPERTS) {
+        // rows past the last expert's are a group of their own, with no K tile: zeros
+        const int e = group_of_slot(P.offsets, P.groups + 1, (int32_t)P.M, BM, ty);
+        if (e < 0) {
+            T.rows = 0;
+            return T;
+        }
+        RowGroup g;
+        if (e < P.groups) {
+            g = row_group(P.offsets, e, (int32_t)P.M);
+        } else {
+            int32_t a = P.offsets[P.groups];
+            a = a < 0 ? 0 : a > (int32_t)P.M ? (int32_t)P.M : a;
+            g = {a, (int32_t)P.M - a};
+            T.count = 0;
+        }
+        const int b = ty - (g.first / BM + e);
+        left = b < 0 ? 0 : (int64_t)g.count - (int64_t)b * BM;
+        T.m0 = g.first + (int64_t)b * BM;
+        T.b0 = e < P.groups ? e * P.N : 0;
+    } else {
+        if (MODE == FP8_EXPERTS_DW) {
+            const int nty = (int)((P.M + BM - 1) / BM), e = ty / nty;
+            ty -= e * nty;
+            const RowGroup g = row_group(P.offsets, e, P.total);
+            T.k0 = g.first / KT + e;
+            T.count = (g.count + KT - 1) / KT;
+            T.out = e * P.M;
+        }
+        T.m0 = (int64_t)ty * BM;
+        left = P.M - T.m0;
+    }
+    T.n0 = (int64_t)tx * BN;
+    T.rows = (int)(left < BM ? left : BM);
+    T.cols = (int)(P.N - T.n0 < BN ? P.N - T.n0 : BN);
+    return T;
+}
+
+// Scale bytes of four neighbouring rows, rows 4 c .. 4 c + 3 of `have` that start at `first`, of K tile `kt` of all the operand's: one load, at any
+// byte.  The array ends with the last K tile's last row; a load that would pass it is moved back.  (Rows past the tile's get some byte.)
+__device__ __forceinline__ uint32_t four_scales(const uint8_t *scales, int64_t rows, int blocks, int kt, int64_t first, int c)
+{
+    struct __attribute__((packed)) Four { uint32_t w; };
+    const int64_t at = kt * rows + first, left = blocks * rows - at;  // (bytes from the first row's on, at least one)
+    const uint8_t *const p = scales + at;
+    if (left >= 64) return reinterpret_cast<const Four *>(p + 4 * c)->w;
+    if (at + left < 4) {  // an operand of one to three bytes
+        uint32_t w = 0;
+        for (int j = 0; j < 4; ++j)
+            if (4 * c + j < left) w |= (uint32_t)p[4 * c + j] << (8 * j);
+        return w;
+    }
+    const int l = (int)left, from = 4 * c + 4 <= l ? 4 * c : l - 4, off = 4 * c - from;
+    return off >= 4 ? 0u : reinterpret_cast<const Four *>(p + from)->w >> (8 * off);
+}
+
+// Two ways to multiply a K tile of two fragments of 16 rows, of which a lane holds 32 codes each.
+//   bf16 outputs: v_mfma_scale_f32_16x16x128_f8f6f4, one instruction, scales included.  It adds the products of a few neighbouring elements with
+//     some 17 bits below the largest of them (so do the other 8-bit forms, 16x16x32 and 32x32x64): the result is off by 1.5e-5 of its norm for normal data, by
+//     up to 1.8e-4 of sum |a||b| of a single block with outliers, where rounding to bf16 takes 1.7e-3 of the norm.
+//   binary32 outputs: the codes become bf16, scale included (v_cvt_scalef32_pk_bf16_fp8: both exact), for v_mfma_f32_16x16x32_bf16, whose sums
+//     are binary32 (1e-7 of the norm), at half the rate and for 32 conversions a lane.
+struct Codes {
+    u32x4_t lo, hi;  // chunks q and q + 4 of a row's eight
+    __device__ __forceinline__ int8v_t all() const
+    {
+        return int8v_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    }
+};
+struct Expanded {
+    bf16x8_t v[4];
+};
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+__device__ __forceinline__ Expanded expand(const Codes &x, uint32_t byte)
+{
+    const float s = scale_of(byte);
+    Expanded r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w = i < 2 ? x.lo[2 * i + h] : x.hi[2 * (i - 2) + h];
+            const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 1);
+            r.v[i][4 * h] = a[0];
+            r.v[i][4 * h + 1] = a[1];
+            r.v[i][4 * h + 2] = b[0];
+            r.v[i][4 * h + 3] = b[1];
+        }
+    return r;
+}
+__device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, const Expanded &a)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], acc, 0, 0, 0);
+}
+
+// n of four columns of one row
+template <int OUT_DT>
+__device__ __forceinline__ void store_four(void *out, int64_t at, const float4v_t &v, int n)
+{
+    if (OUT_DT == NVFP4_F32) {
+        struct __attribute__((packed, aligned(4))) P { u32x4_t w; };
+        float *const p = reinterpret_cast<float *>(out) + at;
+        if (n >= 4) {
+            reinterpret_cast<P *>(p)->w = __builtin_bit_cast(u32x4_t, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) p[i] = v[i];
+        }
+    } else {
+        typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+        struct __attribute__((packed, aligned(2))) P { u32x2_t w; };
+        uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
+        const float2v_t lo = {v[0], v[1]}, hi = {v[2], v[3]};
+        const u32x2_t w = {__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t))};
+        if (n >= 4) {
+            reinterpret_cast<P *>(p)->w = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+}
+
+// Sixteen columns of one row from a lane's accumulators v[4 i + j] = column 4 i + j.  Rows of the output start at any element.
+template <int OUT_DT>
+__device__ __forceinline__ void store_sixteen(void *out, int64_t at, const float (&v)[16], int n)
+{
+    if (OUT_DT == NVFP4_F32) {
+        struct __attribute__((packed, aligned(4))) P { u32x4_t w; };
+        float *const p = reinterpret_cast<float *>(out) + at;
+        if (n >= 16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x4_t w = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+                reinterpret_cast<P *>(p)[i].w = w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < n) p[i] = v[i];
+        }
+    } else {
+        struct __attribute__((packed, aligned(2))) P { u32x4_t w; };
+        uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2v_t f = {v[2 * i], v[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+        }
+        if (n >= 16) {
+            const u32x4_t lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
+            reinterpret_cast<P *>(p)[0].w = lo;
+            reinterpret_cast<P *>(p)[1].w = hi;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+}
+
+}  // namespace f8g
+
+
+}  // namespace nvfp4

@@ -10,115 +10,9 @@
 // four fragments in one dword if these fragments' rows alternate: fragment j (of four) of rows 64 g .. 64 g + 63 has the rows 64 g + 4 c + j,
 // c = 0 .. 15, and the instruction picks byte j.  The first MFMA operand is B's, whose fragments' rows become accumulator rows, so a lane
 // (c, q) ends with 16 consecutive columns 64 g + 16 q .. + 15 of the output rows 64 g' + 4 c + j'.
-#include "experts.h"
+#include "fp8_gemm.h"
 
 namespace nvfp4 {
-namespace f8g {
-
-typedef int int8v_t __attribute__((ext_vector_type(8)));
-typedef float float4v_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float float2v_t __attribute__((ext_vector_type(2)));
-
-constexpr int KT = FP8_BLOCK;
-
-// What a workgroup multiplies: rows m0 .. m0 + rows - 1 of A (and of the output that starts at out) against rows n0 .. n0 + cols - 1 of B,
-// K tiles k0 .. k0 + count - 1; b0 + column is a row of B.  rows <= 0: nothing.
-struct Tile {
-    int64_t m0, n0, b0, out;
-    int rows, cols, k0, count;
-};
-
-template <int MODE>
-__device__ __forceinline__ Tile find_tile(const Fp8GemmArgs &P, unsigned id, int BM, int BN)
-{
-    Tile T;
-    const int ntx = (int)((P.N + BN - 1) / BN);
-    T.k0 = 0;
-    T.count = P.blocks;
-    T.b0 = 0;
-    T.out = 0;
-    int ty = (int)(id / (unsigned)ntx), tx = (int)(id % (unsigned)ntx);
-    int64_t left;
-    if (MODE == FP8_EXPERTS) {
-        // rows past the last expert's are a group of their own, with no K tile: zeros
-        const int e = group_of_slot(P.offsets, P.groups + 1, (int32_t)P.M, BM, ty);
-        if (e < 0) {
-            T.rows = 0;
-            return T;
-        }
-        RowGroup g;
-        if (e < P.groups) {
-            g = row_group(P.offsets, e, (int32_t)P.M);
-        } else {
-            int32_t a = P.offsets[P.groups];
-            a = a < 0 ? 0 : a > (int32_t)P.M ? (int32_t)P.M : a;
-            g = {a, (int32_t)P.M - a};
-            T.count = 0;
-        }
-        const int b = ty - (g.first / BM + e);
-        left = b < 0 ? 0 : (int64_t)g.count - (int64_t)b * BM;
-        T.m0 = g.first + (int64_t)b * BM;
-        T.b0 = e < P.groups ? e * P.N : 0;
-    } else {
-        if (MODE == FP8_EXPERTS_DW) {
-            const int nty = (int)((P.M + BM - 1) / BM), e = ty / nty;
-            ty -= e * nty;
-            const RowGroup g = row_group(P.offsets, e, P.total);
-            T.k0 = g.first / KT + e;
-            T.count = (g.count + KT - 1) / KT;
-            T.out = e * P.M;
-        }
-        T.m0 = (int64_t)ty * BM;
-        left = P.M - T.m0;
-    }
-    T.n0 = (int64_t)tx * BN;
-    T.rows = (int)(left < BM ? left : BM);
-    T.cols = (int)(P.N - T.n0 < BN ? P.N - T.n0 : BN);
-    return T;
-}
-
-// Sixteen columns of one row from a lane's accumulators v[4 i + j] = column 4 i + j.  Rows of the output start at any element.
-template <int OUT_DT>
-__device__ __forceinline__ void store_sixteen(void *out, int64_t at, const float (&v)[16], int n)
-{
-    if (OUT_DT == NVFP4_F32) {
-        struct __attribute__((packed, aligned(4))) P { u32x4_t w; };
-        float *const p = reinterpret_cast<float *>(out) + at;
-        if (n >= 16) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u32x4_t w = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
-                reinterpret_cast<P *>(p)[i].w = w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i < n) p[i] = v[i];
-        }
-    } else {
-        struct __attribute__((packed, aligned(2))) P { u32x4_t w; };
-        uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2v_t f = {v[2 * i], v[2 * i + 1]};
-            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
-        }
-        if (n >= 16) {
-            const u32x4_t lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
-            reinterpret_cast<P *>(p)[0].w = lo;
-            reinterpret_cast<P *>(p)[1].w = hi;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-        }
-    }
-}
-
-}  // namespace f8g
 
 // 128 x 128 tiles: 2 x 2 waves of 64 x 64, two LDS stages of one K tile, filled through registers.
 // LDS: a row's 128 bytes are eight chunks of 16; tile row 64 g + 4 c + j stands at position 64 g + 16 j + c, its chunk h at slot
@@ -161,17 +55,6 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
             *reinterpret_cast<u32x4_t *>(lds + st * STAGE + BM * KT + to[u]) = gb[u];
         }
     };
-    // the bytes of rows 4 c .. 4 c + 3 of the wave's 64, clamped one by one at the edge
-    auto scales = [&](const uint8_t *s, int64_t rows, int64_t first, int have, int kt) -> uint32_t {
-        const uint8_t *p = s + (int64_t)(T.k0 + kt) * rows + first;
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = 4 * c + j < have ? 4 * c + j : have - 1;
-            w |= (uint32_t)p[r < 0 ? 0 : r] << (8 * j);
-        }
-        return w;
-    };
     float4v_t acc[4][4];
 #pragma unroll
     for (int a = 0; a < 4; ++a)
@@ -186,23 +69,36 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
     for (int kt = 0; kt < T.count; ++kt) {
         const bool more = kt + 1 < T.count;
         if (more) fetch(kt + 1);
-        const uint32_t sa = scales(P.A_scales, P.a_rows, T.m0 + ma, T.rows - ma, kt);
-        const uint32_t sb = scales(P.B_scales, P.b_rows, T.b0 + T.n0 + nb, T.cols - nb, kt);
+        const uint32_t sa = four_scales(P.A_scales, P.a_rows, P.blocks, T.k0 + kt, T.m0 + ma, c);
+        const uint32_t sb = four_scales(P.B_scales, P.b_rows, P.blocks, T.k0 + kt, T.b0 + T.n0 + nb, c);
         const uint8_t *const base = lds + (kt & 1) * STAGE + c * KT, *const A = base + wm * 64 * KT, *const B = base + (BM + wn * 64) * KT;
         const int s0 = (q ^ (c >> 1)) << 4, s1 = ((q + 4) ^ (c >> 1)) << 4;
-        int8v_t fa[4], fb[4];
+        auto read = [&](const uint8_t *p, int j) -> Codes {
+            return {*reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s0), *reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s1)};
+        };
+        if constexpr (OUT_DT == NVFP4_F32) {
+            Expanded fa[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const u32x4_t a0 = *reinterpret_cast<const u32x4_t *>(A + 16 * j * KT + s0), a1 = *reinterpret_cast<const u32x4_t *>(A + 16 * j * KT + s1);
-            const u32x4_t b0 = *reinterpret_cast<const u32x4_t *>(B + 16 * j * KT + s0), b1 = *reinterpret_cast<const u32x4_t *>(B + 16 * j * KT + s1);
-            fa[j] = int8v_t{(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-            fb[j] = int8v_t{(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-        }
+            for (int a = 0; a < 4; ++a) fa[a] = expand(read(A, a), (sa >> (8 * a)) & 255);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const Expanded fb = expand(read(B, b), (sb >> (8 * b)) & 255);
+#pragma unroll
+                for (int a = 0; a < 4; ++a) multiply(acc[a][b], fb, fa[a]);
+            }
+        } else {
+            int8v_t fa[4], fb[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                fa[j] = read(A, j).all();
+                fb[j] = read(B, j).all();
+            }
 #define NVFP4_F8_MFMA(a, b) acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[b], fa[a], acc[a][b], 0, 0, b, sb, a, sa);
 #define NVFP4_F8_MFMA_ROW(a) NVFP4_F8_MFMA(a, 0) NVFP4_F8_MFMA(a, 1) NVFP4_F8_MFMA(a, 2) NVFP4_F8_MFMA(a, 3)
-        NVFP4_F8_MFMA_ROW(0) NVFP4_F8_MFMA_ROW(1) NVFP4_F8_MFMA_ROW(2) NVFP4_F8_MFMA_ROW(3)
+            NVFP4_F8_MFMA_ROW(0) NVFP4_F8_MFMA_ROW(1) NVFP4_F8_MFMA_ROW(2) NVFP4_F8_MFMA_ROW(3)
 #undef NVFP4_F8_MFMA_ROW
 #undef NVFP4_F8_MFMA
+        }
         if (more) stash((kt + 1) & 1);
         __syncthreads();
     }
@@ -219,16 +115,19 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
 }
 
 template <int MODE>
-static hipError_t launch(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+static hipError_t launch_tiles(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     constexpr int BM = 128, BN = 128, LDS = 2 * (BM + BN) * FP8_BLOCK;
-    const int64_t ntx = (P.N + BN - 1) / BN, nty = (P.M + BM - 1) / BM;
-    const int64_t tiles = ntx * (MODE == FP8_EXPERTS ? P.M / BM + P.groups + 1 : MODE == FP8_EXPERTS_DW ? nty * P.groups : nty);
     auto *k = out_dt == NVFP4_F32 ? fp8_gemm_kernel<MODE, NVFP4_F32> : fp8_gemm_kernel<MODE, NVFP4_BF16>;
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (e != hipSuccess) return e;
-    k<<<dim3((unsigned)tiles), 256, LDS, st>>>(P);
+    k<<<dim3((unsigned)f8g::tiles<MODE>(P, BM, BN)), 256, LDS, st>>>(P);
     return hipGetLastError();
+}
+
+template <int MODE>
+static hipError_t launch(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+{
+    if (MODE != FP8_EXPERTS_DW && fp8_gemm_is_thin(P, MODE)) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
+    return launch_tiles<MODE>(P, out_dt, st);
 }
 
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
