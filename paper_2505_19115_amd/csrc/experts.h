@@ -73,6 +73,8 @@ struct Fp8GemmArgs {
 };
 bool fp8_gemm_is_thin(const Fp8GemmArgs &P, int mode);  // few rows: of all, or of each expert on average
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
+bool fp8_gemm_is_wide(const Fp8GemmArgs &P, int mode);  // bf16 outputs on 256 x 256 tiles
+hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, hipStream_t st);
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 
 // Routing

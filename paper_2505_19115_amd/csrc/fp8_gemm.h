@@ -1,6 +1,7 @@
 // What the kernels of 8-bit products share: which rows and K tiles a workgroup's tile covers, scale bytes, fragments, and the way out.
 #pragma once
 #include "experts.h"
+#include "kernels.h"
 
 namespace nvfp4 {
 namespace f8g {
@@ -38,7 +39,8 @@ __device__ __forceinline__ Tile find_tile(const Fp8GemmArgs &P, unsigned id, int
     T.count = P.blocks;
     T.b0 = 0;
     T.out = 0;
-    int ty = (int)(id / (unsigned)ntx), tx = (int)(id % (unsigned)ntx);
+    int ty, tx;
+    tile_coords((int)id, ntx, (int)(gridDim.x / (unsigned)ntx), ty, tx);
     int64_t left;
     if (MODE == FP8_EXPERTS) {
         // rows past the last expert's are a group of their own, with no K tile: zeros

@@ -127,6 +127,7 @@ template <int MODE>
 static hipError_t launch(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     if (MODE != FP8_EXPERTS_DW && fp8_gemm_is_thin(P, MODE)) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
+    if (out_dt == NVFP4_BF16 && fp8_gemm_is_wide(P, MODE)) return launch_fp8_gemm_wide(P, (Fp8Mode)MODE, st);
     return launch_tiles<MODE>(P, out_dt, st);
 }
 
