@@ -2,14 +2,18 @@
 // wave per SIMD).  A K tile is 64 MFMAs a wave, 32 cycles each, and 128 KB out of the LDS for the four of them, half of what it delivers
 // in that time.
 //
-// LDS: two stages of one K tile, 32 KB of each operand, placed as in fp8_gemm.hip (row 64 g + 4 c + j at position 64 g + 16 j + c, chunk h at slot h ^ (c / 2)),
-// written by direct global -> LDS loads whose lanes choose which chunk they fetch.  Rows past the edge are clamped to the last one.
+// LDS: two stages of one K tile, 32 KB of each operand, placed as in fp8_gemm.hip (row 64 g + 4 c + j at position 64 g + 16 j + c, chunk h at slot h ^ (c / 2)), and
+// its 512 scale bytes, a dword each in the rows' order, so that a lane's four fragments' come in one read.  All of it is written by direct global ->
+// LDS loads (scales byte by byte: they start anywhere), so that the loads in flight can be counted.  Rows past the edge are clamped to the last one.
 //
 // A K tile in quarters, halves of A against halves of B, a half's registers read again as soon as its last quarter is done; of B the half that
 // the tile before ended without comes first (P, then Q):
-//     A0 x P   while Q is read             A0 x Q   while A1 is read
-//     ONE barrier, with every load of tile kt + 1 landed and this tile's stage read by every wave
-//     A1 x Q   while A0 of kt + 1 is read  A1 x P   while Q of kt + 1 is read, the next tile's P;    tile kt + 2 is requested meanwhile
+//     A0 x P   while Q is read             A0 x Q   while A1 is read            a barrier: A0, P and scales of kt + 1 have landed
+//     A1 x Q   while A0 of kt + 1 is read  A1 x P   while its P and scales are  a barrier: Q and A1 of kt + 1 have landed
+// A barrier also says that every wave has read what the two quarters before it read, whose place the loads for two K tiles on then take: A0, P and
+// scales in a tile's first quarter, Q and A1 in its third.  So a load has a K tile and a quarter at least; with the loads behind the first barrier only,
+// three quarters, 4096 x 4096 x 11008 took 167 us.  Past the last K tile the loads repeat one piece of the first, so that
+// the counts hold.
 #include <type_traits>
 
 #include "fp8_gemm.h"
@@ -18,17 +22,15 @@ namespace nvfp4 {
 namespace f8w {
 
 constexpr int BM = 256, BN = 256, KT = FP8_BLOCK;
-constexpr int STAGE = (BM + BN) * KT, LDS_BYTES = 2 * STAGE;
+constexpr int STAGE = (BM + BN) * KT, SCALES = (BM + BN) * 4, SCALES0 = 2 * STAGE, LDS_BYTES = SCALES0 + 2 * SCALES;
+constexpr int FIRST = 10, SECOND = 8;  // loads of a wave and K tile: A0, P and scales; Q and A1
 
 // As assembly, so that the 64 accumulators stay where they are (gemm_mx.hip).  What the compiler does not know about it: an operand must not have been
 // written by the vector ALU in the two instructions before (they come from LDS reads), and the last result must not be read for 11 wait
-// states.  BA, BB: bytes of the scale registers.
-template <int BB, int BA>
+// states.
 __device__ __forceinline__ void mfma(f8g::float4v_t &acc, const f8g::int8v_t &b, const f8g::int8v_t &a, uint32_t sb, uint32_t sa)
 {
-    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
-                 : "+a"(acc)
-                 : "v"(b), "v"(a), "v"(sb), "v"(sa), "n"(BB & 1), "n"(BA & 1), "n"(BB >> 1), "n"(BA >> 1));
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(acc) : "v"(b), "v"(a), "v"(sb), "v"(sa));
 }
 
 // Assembly because the compiler takes a direct-to-LDS load for a possible writer of all of the LDS and would wait for it before the next LDS
@@ -37,6 +39,12 @@ template <int TO>
 __device__ __forceinline__ void load(uint32_t dst, uint32_t off, const uint8_t *base)
 {
     asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" : : "s"(dst), "n"(TO), "v"(off), "s"(base) : "memory", "scc", "m0");
+}
+
+template <int TO>
+__device__ __forceinline__ void load_byte(uint32_t dst, uint32_t off, const uint8_t *base)
+{
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %2, %3" : : "s"(dst), "n"(TO), "v"(off), "s"(base) : "memory", "scc", "m0");
 }
 
 template <int I, int N, class F>
@@ -62,22 +70,60 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     if (T.rows <= 0) return;
     const int64_t pitch = (int64_t)P.blocks * KT;
 
-    // ---- global -> LDS: instruction u of a wave fills positions 64 wave + 8 u .. + 7
-    uint32_t offA[8], offB[8];
+    // ---- global -> LDS: instruction u of four of a half fills 8 of the wave's 32 positions of it.  (Half h: positions 64 h .. + 63 of
+    // each 128.)
+    uint32_t offA[8], offB[8];  // [half][u]
+    const int first = 128 * (wave >> 1), second = 32 * (wave & 1);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        const int at = (u & 1) * 8 + (lane >> 3), row = 64 * wave + 4 * at + (u >> 1), chunk = (lane & 7) ^ (at >> 1);
-        offA[u] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + chunk * 16;
-        offB[u] = (uint32_t)((row < T.cols ? row : T.cols - 1) * pitch) + chunk * 16;
+    for (int i = 0; i < 8; ++i) {
+        const int in = second + 8 * (i & 3) + (lane >> 3), at = in & 15, row = first + 64 * (i >> 2) + 4 * at + (in >> 4), chunk = (lane & 7) ^ (at >> 1);
+        offA[i] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + chunk * 16;
+        offB[i] = (uint32_t)((row < T.cols ? row : T.cols - 1) * pitch) + chunk * 16;
     }
+    const int srow = wave * 64 + lane;
+    uint32_t offSA = srow < T.rows ? srow : T.rows - 1, offSB = srow < T.cols ? srow : T.cols - 1;
     auto uniform = [](const uint8_t *p) -> const uint8_t * {
         const uint64_t v = reinterpret_cast<uint64_t>(p);
         const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
         return reinterpret_cast<const uint8_t *>(((uint64_t)hi << 32) | lo);
     };
-    const uint8_t *pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT), *pB = uniform(P.B + (T.b0 + T.n0) * pitch + (int64_t)T.k0 * KT);  // next to be requested
+    // K tile that is requested next
+    const uint8_t *pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT), *pB = uniform(P.B + (T.b0 + T.n0) * pitch + (int64_t)T.k0 * KT);
+    const uint8_t *pSA = uniform(P.A_scales + T.k0 * P.a_rows + T.m0), *pSB = uniform(P.B_scales + T.k0 * P.b_rows + T.b0 + T.n0);
+    int64_t step = KT, stepSA = P.a_rows, stepSB = P.b_rows;
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
-    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)lds + wave * 8192);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds, dst = __builtin_amdgcn_readfirstlane(lds0 + (first + second) * KT),
+                   dstS = __builtin_amdgcn_readfirstlane(lds0 + f8w::SCALES0 + wave * 256);
+    // load i of a K tile: of the first ones (A0, P = half ST of B, scales) and of the second (Q, A1)
+    auto request_first = [&](auto st, auto i) {
+        constexpr int S = decltype(st)::value, I = decltype(i)::value;
+        if constexpr (I < 4) f8w::load<S * STAGE + I * 1024>(dst, offA[I], pA);
+        else if constexpr (I < 8) f8w::load<S * STAGE + BM * KT + S * 8192 + (I - 4) * 1024>(dst, offB[4 * S + I - 4], pB);
+        else if constexpr (I == 8) f8w::load_byte<S * f8w::SCALES>(dstS, offSA, pSA);
+        else f8w::load_byte<S * f8w::SCALES + 4 * BM>(dstS, offSB, pSB);
+    };
+    auto request_second = [&](auto st, auto i) {
+        constexpr int S = decltype(st)::value, I = decltype(i)::value;
+        if constexpr (I < 4) f8w::load<S * STAGE + BM * KT + (1 - S) * 8192 + I * 1024>(dst, offB[4 * (1 - S) + I], pB);
+        else f8w::load<S * STAGE + 8192 + (I - 4) * 1024>(dst, offA[I], pA);
+    };
+    auto advance = [&]() {
+        pA += step;
+        pB += step;
+        pSA += stepSA;
+        pSB += stepSB;
+    };
+    auto past_end = [&]() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) offA[i] = offB[i] = 0;
+        offSA = offSB = 0;
+        pA = P.A;
+        pB = P.B;
+        pSA = P.A_scales;
+        pSB = P.B_scales;
+        step = stepSA = stepSB = 0;
+    };
+
     // ---- LDS -> registers: fragment f of the wave's 128 rows of an operand
     const int s0 = (q ^ (c >> 1)) << 4;
     const uint8_t *baseA[2][2], *baseB[2][2];  // [stage][half of the row]
@@ -102,40 +148,28 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
         for (int b = 0; b < 8; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // scale bytes of the wave's rows in a K tile
-    struct Scales {
-        uint32_t a[2], b[2];
+    // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
+    u32x4_t SA[2][2], SB[2][2];
+    const uint8_t *baseSA = lds + f8w::SCALES0 + (wm * 128 + 4 * c) * 4, *baseSB = lds + f8w::SCALES0 + (BM + wn * 128 + 4 * c) * 4;
+    auto read_scales = [&](int st, int i) {
+        (i < 2 ? SA[st][i & 1] : SB[st][i & 1]) = *reinterpret_cast<const u32x4_t *>((i < 2 ? baseSA : baseSB) + st * f8w::SCALES + (i & 1) * 256);
     };
-    const int64_t sa0 = T.m0 + (wm * 128 < T.rows ? wm * 128 : 0), sb0 = T.b0 + T.n0 + (wn * 128 < T.cols ? wn * 128 : 0);
-    const int sa1 = wm * 128 + 64 < T.rows ? 64 : 0, sb1 = wn * 128 + 64 < T.cols ? 64 : 0;  // (parts past the edge: the first bytes, for results that nobody stores)
-    auto scales = [&](int kt) -> Scales {
-        return {{four_scales(P.A_scales, P.a_rows, P.blocks, T.k0 + kt, sa0, c), four_scales(P.A_scales, P.a_rows, P.blocks, T.k0 + kt, sa0 + sa1, c)},
-                {four_scales(P.B_scales, P.b_rows, P.blocks, T.k0 + kt, sb0, c), four_scales(P.B_scales, P.b_rows, P.blocks, T.k0 + kt, sb0 + sb1, c)}};
-    };
-    auto there = [](Scales &s) { asm volatile("" : "+v"(s.a[0]), "+v"(s.a[1]), "+v"(s.b[0]), "+v"(s.b[1])); };
-    auto request = [&](auto st, auto i) {  // load i of 16 of a K tile
-        constexpr int S = decltype(st)::value, U = decltype(i)::value & 7;
-        if constexpr (decltype(i)::value < 8) {
-            f8w::load<S * STAGE + U * 1024>(dst, offA[U], pA);
-        } else {
-            f8w::load<S * STAGE + BM * KT + U * 1024>(dst, offB[U], pB);
-        }
-    };
-    Scales now, next;
+    // everything but the last n loads has landed and all of the wave's LDS reads are done; then the same of every wave
+#define NVFP4_F8W_BARRIER(n)                                                    \
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(n) : "memory"); \
+    __builtin_amdgcn_s_barrier();                                               \
+    asm volatile("" ::: "memory");
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
     if (T.count > 0) {
-        f8w::each<0, 16>([&](auto i) { request(std::integral_constant<int, 0>{}, i); });
-        pA += KT;
-        pB += KT;
-        now = scales(0);
-        if (T.count > 1) {
-            f8w::each<0, 16>([&](auto i) { request(std::integral_constant<int, 1>{}, i); });
-            pA += KT;
-            pB += KT;
-            next = scales(1);
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        there(now);
-        __syncthreads();
+        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I0{}, i); });
+        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I0{}, i); });
+        advance();
+        if (T.count < 2) past_end();
+        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I1{}, i); });
+        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I1{}, i); });
+        advance();
+        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
 #pragma unroll
         for (int f = 0; f < 4; ++f)
 #pragma unroll
@@ -143,68 +177,63 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                 read_a(0, f, h);
                 read_b(0, f, h);
             }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) read_scales(0, i);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
     int kt = 0;
-    // stage ST; P: the half of B that is there already
+    // stage ST, which is also the half P of B
     auto tile = [&](auto stage) {
-        constexpr int ST = decltype(stage)::value, Pb = ST, Qb = 1 - ST;
-        // (the scales may just have been copied from register to register: two instructions between that and the MFMAs)
-        asm volatile("s_nop 1" : "+v"(now.a[0]), "+v"(now.a[1]), "+v"(now.b[0]), "+v"(now.b[1]));
+        constexpr int ST = decltype(stage)::value;
+        using HP = std::integral_constant<int, ST>;
+        using HQ = std::integral_constant<int, 1 - ST>;
+        if (kt + 2 >= T.count) past_end();
         __builtin_amdgcn_sched_barrier(0);
-        auto one = [&](auto ia, auto ib) {
-            constexpr int a = decltype(ia)::value, b = decltype(ib)::value;
-            f8w::mfma<(b & 3), (a & 3)>(acc[a][b], B[b].all(), A[a].all(), now.b[b >> 2], now.a[a >> 2]);
-        };
         // MFMA j of a quarter: along a row of tiles and back along the next, one operand changes at a time
         auto quarter = [&](auto ha, auto hb, auto &&between) {
             f8w::each<0, 16>([&](auto j) {
                 constexpr int J = decltype(j)::value, r = J >> 2, i = r & 1 ? 3 - (J & 3) : J & 3;
-                one(std::integral_constant<int, 4 * decltype(ha)::value + r>{}, std::integral_constant<int, 4 * decltype(hb)::value + i>{});
+                constexpr int a = 4 * decltype(ha)::value + r, b = 4 * decltype(hb)::value + i;
+                f8w::mfma(acc[a][b], B[b].all(), A[a].all(), SB[ST][b >> 2][b & 3], SA[ST][a >> 2][a & 3]);
                 __builtin_amdgcn_sched_barrier(0);
                 between(j);
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
-        using H0 = std::integral_constant<int, 0>;
-        using H1 = std::integral_constant<int, 1>;
-        using HP = std::integral_constant<int, Pb>;
-        using HQ = std::integral_constant<int, Qb>;
-        quarter(H0{}, HP{}, [&](auto j) {
+        quarter(I0{}, HP{}, [&](auto j) {
             constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_b(ST, 4 * Qb + (J >> 1), J & 1);
+            if constexpr (J < 8) read_b(ST, 4 * (1 - ST) + (J >> 1), J & 1);
+            if constexpr (J >= 16 - f8w::FIRST) request_first(stage, std::integral_constant<int, J - (16 - f8w::FIRST)>{});
         });
-        quarter(H0{}, HQ{}, [&](auto j) {
+        quarter(I0{}, HQ{}, [&](auto j) {
             constexpr int J = decltype(j)::value;
             if constexpr (J < 8) read_a(ST, 4 + (J >> 1), J & 1);
         });
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        there(next);
-        const bool more = kt + 2 < T.count;
-        Scales later = next;
-        if (more) later = scales(kt + 2);
+        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
         __builtin_amdgcn_sched_barrier(0);
-        quarter(H1{}, HQ{}, [&](auto j) {
+        quarter(I1{}, HQ{}, [&](auto j) {
             constexpr int J = decltype(j)::value;
             if constexpr (J < 8) read_a(1 - ST, J >> 1, J & 1);
-            if (more) request(stage, j);
+            if constexpr (J >= 8) request_second(stage, std::integral_constant<int, J - 8>{});
         });
-        quarter(H1{}, HP{}, [&](auto j) {
+        advance();
+        quarter(I1{}, HP{}, [&](auto j) {
             constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_b(1 - ST, 4 * Qb + (J >> 1), J & 1);
+            if constexpr (J < 8) read_b(1 - ST, 4 * (1 - ST) + (J >> 1), J & 1);
+            if constexpr (J >= 8 && J < 12) read_scales(1 - ST, J - 8);
         });
-        pA += KT;
-        pB += KT;
-        now = next;
-        next = later;
+        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
         ++kt;
     };
     while (kt + 2 <= T.count) {
-        tile(std::integral_constant<int, 0>{});
-        tile(std::integral_constant<int, 1>{});
+        tile(I0{});
+        tile(I1{});
     }
-    if (kt < T.count) tile(std::integral_constant<int, 0>{});
+    if (kt < T.count) tile(I0{});
+#undef NVFP4_F8W_BARRIER
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the loads past the end, before the workgroup's LDS is another's)
     asm volatile("s_nop 15" ::: "memory");
 #pragma unroll
     for (int a = 0; a < 8; ++a)
