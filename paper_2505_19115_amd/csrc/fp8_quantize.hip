@@ -13,62 +13,59 @@ namespace f8 {
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
-// Eight neighbouring elements as binary32 bits.  Rows start at any multiple of an element: the memory pipe takes wide loads at any such
-// address (ragged pitches cost requests, not instructions).
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Eight neighbouring elements as they came, in W words.  Rows start at any multiple of an element: the memory pipe takes wide loads at any such
+// address (ragged pitches cost requests, not instructions).  Magnitudes are compared as integers, NaN above infinity above every number,
+// bf16 ones two at a time.
 template <int DT>
 struct Eight {
-    uint32_t v[8];
+    static constexpr bool HALF = DT == NVFP4_BF16;
+    static constexpr int W = HALF ? 4 : 8, ESZ = HALF ? 2 : 4;
+    uint32_t w[W];
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0;
+        for (int i = 0; i < W; ++i) w[i] = 0;
     }
-    __device__ __forceinline__ void load(const void *row, int64_t col)
+    __device__ __forceinline__ void load(const uint8_t *p)
     {
-        if (DT == NVFP4_BF16) {
-            struct __attribute__((packed, aligned(2))) P { u32x4_t w; };
-            const u32x4_t w = reinterpret_cast<const P *>(reinterpret_cast<const uint16_t *>(row) + col)->w;
+        struct __attribute__((packed, aligned(ESZ))) P { u32x4_t w; };
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = w[i] << 16;
-                v[2 * i + 1] = w[i] & 0xFFFF0000u;
-            }
-        } else {
-            struct __attribute__((packed, aligned(4))) P { u32x4_t w; };
-            const P *p = reinterpret_cast<const P *>(reinterpret_cast<const float *>(row) + col);
-            const u32x4_t lo = p[0].w, hi = p[1].w;
+        for (int i = 0; i < W / 4; ++i) {
+            const u32x4_t v = reinterpret_cast<const P *>(p)[i].w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = lo[i];
-                v[4 + i] = hi[i];
-            }
+            for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
         }
     }
-    __device__ __forceinline__ void load_some(const void *row, int64_t col, int n)
+    __device__ __forceinline__ void load_some(const uint8_t *p, int n)
     {
+        zero();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            v[i] = i >= n ? 0u : DT == NVFP4_BF16 ? (uint32_t)reinterpret_cast<const uint16_t *>(row)[col + i] << 16 : reinterpret_cast<const uint32_t *>(row)[col + i];
+            if (i < n) {
+                if (HALF) w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i & 1));
+                else w[i % W] = reinterpret_cast<const uint32_t *>(p)[i];
+            }
     }
-    __device__ __forceinline__ void load_upto(const void *row, int64_t col, int64_t cols)
+    // binary32 bits of element i
+    __device__ __forceinline__ uint32_t bits(int i) const { return HALF ? (i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) : w[i % W]; }
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float(bits(i)); }
+    __device__ __forceinline__ static uint32_t magnitudes(uint32_t v) { return v & (HALF ? 0x7FFF7FFFu : 0x7FFFFFFFu); }
+    __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b)
     {
-        if (col + 8 <= cols) load(row, col);
-        else if (col < cols) load_some(row, col, (int)(cols - col));
-        else zero();
+        typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+        return HALF ? __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a), __builtin_bit_cast(u16x2_t, b))) : umax(a, b);
+    }
+    // the largest magnitude's bits
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        uint32_t m = magnitudes(w[0]);
+#pragma unroll
+        for (int i = 1; i < W; ++i) m = larger(m, magnitudes(w[i]));
+        return HALF ? umax(m << 16, m & 0xFFFF0000u) : m;
     }
 };
-
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
-// (magnitudes as integers: NaN above infinity above every number)
-template <int DT>
-__device__ __forceinline__ uint32_t largest(const Eight<DT> &x)
-{
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = umax(m, x.v[i] & 0x7FFFFFFFu);
-    return m;
-}
 
 // maximum over the 16 lanes of a row of lanes
 __device__ __forceinline__ uint32_t max16(uint32_t m)
@@ -92,22 +89,58 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t m)
 // 2^-e; of a block that is not finite NaN, which makes every code one
 __device__ __forceinline__ float inverse_scale(uint32_t m, uint32_t byte) { return __uint_as_float(m >= NOT_FINITE ? 0x7FC00000u : (254u - byte) << 23); }
 
-__device__ __forceinline__ uint32_t four_codes(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float q)
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, float q)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(a) * q, __uint_as_float(b) * q, 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(c) * q, __uint_as_float(d) * q, w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * q, b * q, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * q, d * q, w, true);
     return (uint32_t)w;
+}
+template <int DT>
+__device__ __forceinline__ u32x2_t eight_codes(const Eight<DT> &x, float q)
+{
+    return u32x2_t{four_codes(x.value(0), x.value(1), x.value(2), x.value(3), q), four_codes(x.value(4), x.value(5), x.value(6), x.value(7), q)};
 }
 
 }  // namespace f8
 
-// Row of x behind row r, -1 for none
-__device__ __forceinline__ int64_t source_row(const Fp8QuantArgs &P, int64_t r)
+// Elements col .. col + 7 of N rows r0, r0 + step, ..., of which there are `have` (rows past these, and rows that an order does not name, are zeros).
+// Loads of whole pieces do not branch: a row that is not there reads the first one instead.
+template <int DT, int N>
+__device__ __forceinline__ void load_rows(const Fp8QuantArgs &P, f8::Eight<DT> (&x)[N], int64_t r0, int have, int64_t col, bool whole)
 {
-    if (!P.order) return r;
-    const int32_t pair = P.order[r];
-    const int64_t at = pair < 0 ? -1 : pair / P.top_k;
-    return at < P.x_rows ? at : -1;
+    constexpr int ESZ = f8::Eight<DT>::ESZ;
+    const uint8_t *const base = reinterpret_cast<const uint8_t *>(P.x) + col * ESZ;
+    if (P.order ? P.x_rows == 0 : false) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i].zero();
+        return;
+    }
+    int64_t src[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        src[i] = i < have ? r0 + i : -1;
+        if (P.order) {
+            const int32_t pair = P.order[i < have ? r0 + i : 0];
+            const int64_t at = pair / P.top_k;
+            src[i] = i < have && pair >= 0 && at < P.x_rows ? at : -1;
+        }
+    }
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i].load(base + (src[i] < 0 ? 0 : src[i]) * P.ld * ESZ);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < f8::Eight<DT>::W; ++k) x[i].w[k] = src[i] < 0 ? 0u : x[i].w[k];
+    } else {
+        const int64_t left = P.cols - col;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (src[i] < 0 || left <= 0) x[i].zero();
+            else if (left >= 8) x[i].load(base + src[i] * P.ld * ESZ);
+            else x[i].load_some(base + src[i] * P.ld * ESZ, (int)left);
+        }
+    }
 }
 
 // Rows alone.  16 lanes hold a block, a wave four groups of RPG consecutive rows each: as many loads in flight, and their scale bytes are
@@ -118,23 +151,17 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs P, 
     using namespace f8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane & 15;
     const unsigned up = blockIdx.x / across;
-    const int kb = (int)(blockIdx.x - up * across) * 4 + wave;
+    const int kb = __builtin_amdgcn_readfirstlane((int)(blockIdx.x - up * across) * 4 + wave);
     if (kb >= blocks) return;
     const int64_t r0 = ((int64_t)up * 4 + (lane >> 4)) * RPG;
     const int64_t col = (int64_t)kb * FP8_BLOCK + in * 8;
     Eight<DT> x[RPG];
-#pragma unroll
-    for (int i = 0; i < RPG; ++i) {
-        const int64_t src = r0 + i < rows ? source_row(P, r0 + i) : -1;
-        if (src < 0) x[i].zero();
-        else x[i].load_upto(reinterpret_cast<const uint8_t *>(P.x) + src * P.ld * (DT == NVFP4_BF16 ? 2 : 4), col, P.cols);
-    }
+    load_rows<DT, RPG>(P, x, r0, (int)(rows - r0 < RPG ? rows - r0 : RPG), col, (int64_t)(kb + 1) * FP8_BLOCK <= P.cols);
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < RPG; ++i) {
-        const uint32_t m = max16(largest(x[i])), byte = scale_byte(m);
-        const float q = inverse_scale(m, byte);
-        const u32x2_t w = {four_codes(x[i].v[0], x[i].v[1], x[i].v[2], x[i].v[3], q), four_codes(x[i].v[4], x[i].v[5], x[i].v[6], x[i].v[7], q)};
+        const uint32_t m = max16(x[i].largest()), byte = scale_byte(m);
+        const u32x2_t w = eight_codes(x[i], inverse_scale(m, byte));
         if (r0 + i < rows) *reinterpret_cast<u32x2_t *>(P.codes_r + (r0 + i) * blocks * FP8_BLOCK + col) = w;
         if (in == i) mine = byte;
     }
@@ -173,35 +200,31 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
     if (count <= 0) return;
     const int64_t col = (int64_t)tile * FP8_BLOCK + cg * 8;
     Eight<DT> x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t src = rg * 8 + i < count ? source_row(P, row0 + rg * 8 + i) : -1;
-        if (src < 0) x[i].zero();
-        else x[i].load_upto(reinterpret_cast<const uint8_t *>(P.x) + src * P.ld * (DT == NVFP4_BF16 ? 2 : 4), col, P.cols);
-    }
+    load_rows<DT, 8>(P, x, row0 + rg * 8, count - rg * 8, col, (int64_t)(tile + 1) * FP8_BLOCK <= P.cols);
     // columns' largest magnitudes: of the thread's rows, of the wave's, of all
-    uint32_t colmax[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        uint32_t m = 0;
+    for (int j = 0; j < Eight<DT>::W; ++j) {
+        uint32_t m = Eight<DT>::magnitudes(x[0].w[j]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = umax(m, x[i].v[j] & 0x7FFFFFFFu);
-        m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-        m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
-        colmax[j] = m;
-    }
-    if (lane < 16) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top[wave][cg * 8 + j] = colmax[j];
+        for (int i = 1; i < 8; ++i) m = Eight<DT>::larger(m, Eight<DT>::magnitudes(x[i].w[j]));
+        m = Eight<DT>::larger(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = Eight<DT>::larger(m, (uint32_t)__shfl_xor((int)m, 32));
+        if (lane < 16) {
+            if (Eight<DT>::HALF) {
+                top[wave][cg * 8 + (2 * j & 7)] = m << 16;
+                top[wave][cg * 8 + (2 * j & 7) + 1] = m & 0xFFFF0000u;
+            } else {
+                top[wave][cg * 8 + j] = m;
+            }
+        }
     }
     if (ROWS) {
         const int64_t rows = P.batch * P.rows, pitch = (int64_t)col_tiles * FP8_BLOCK;
         uint32_t mine = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t m = max16(largest(x[i])), byte = scale_byte(m);
-            const float q = inverse_scale(m, byte);
-            const u32x2_t w = {four_codes(x[i].v[0], x[i].v[1], x[i].v[2], x[i].v[3], q), four_codes(x[i].v[4], x[i].v[5], x[i].v[6], x[i].v[7], q)};
+            const uint32_t m = max16(x[i].largest()), byte = scale_byte(m);
+            const u32x2_t w = eight_codes(x[i], inverse_scale(m, byte));
             if (rg * 8 + i < count) *reinterpret_cast<u32x2_t *>(P.codes_r + (row0 + rg * 8 + i) * pitch + col) = w;
             if (cg == i) mine = byte;
         }
@@ -215,7 +238,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
         for (int w = 0; w < 4; ++w) m = umax(m, top[w][cg * 8 + j]);
         const uint32_t byte = scale_byte(m);
         const float q = inverse_scale(m, byte);
-        const u32x2_t w = {four_codes(x[0].v[j], x[1].v[j], x[2].v[j], x[3].v[j], q), four_codes(x[4].v[j], x[5].v[j], x[6].v[j], x[7].v[j], q)};
+        const u32x2_t w = {four_codes(x[0].value(j), x[1].value(j), x[2].value(j), x[3].value(j), q), four_codes(x[4].value(j), x[5].value(j), x[6].value(j), x[7].value(j), q)};
         *reinterpret_cast<u32x2_t *>(turned + (cg * 8 + j) * PITCH + rg * 8) = w;
     }
     const int64_t out_rows = P.batch * P.cols, out0 = matrix * P.cols + (int64_t)tile * FP8_BLOCK, pitch = (int64_t)slots * FP8_BLOCK;
