@@ -685,13 +685,31 @@ def quant_noise(x: torch.Tensor, q, axis: int = 1, fmt: Format = NVFP4, out: tor
 # ---- 8-bit linear layers and mixtures of experts
 
 FP8_BLOCK = 128
+# (Of a call's 8 us on the host the launch takes 3.4 and an output tensor 1.3 at best, with its sizes as arguments; the checks below are written to
+# cost little of the rest.)
+_E4M3, _I32, _U8 = torch.float8_e4m3fn, torch.int32, torch.uint8
 
 
-class Fp8(NamedTuple):
+class Fp8:
     """An 8-bit operand of a [rows, K] tensor: codes [rows, P] (float8_e4m3fn, P the next multiple of 128 of K, zero past K) and scales
-    [P / 128, rows] (uint8, 2^(byte - 127))."""
-    codes: torch.Tensor
-    scales: torch.Tensor
+    [P / 128, rows] (uint8, 2^(byte - 127)).  Checked here, so that the products need not."""
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dtype is not _E4M3 or scales.dtype is not _U8 or not codes.is_contiguous() or not scales.is_contiguous():
+            raise TypeError("an operand: contiguous float8_e4m3fn codes and uint8 scales")
+        if not codes.is_cuda or not scales.is_cuda:
+            raise ValueError("tensors must live on the GPU")
+        if codes.dim() != 2 or codes.shape[1] % FP8_BLOCK or scales.shape != (codes.shape[1] // FP8_BLOCK, codes.shape[0]):
+            raise ValueError("an operand: codes [rows, 128 S] with scales [S, rows]")
+        self.codes, self.scales = codes, scales
+
+
+def _fp8_empty(rows: int, blocks: int, device: torch.device) -> Fp8:
+    q = Fp8.__new__(Fp8)
+    q.codes = torch.empty(rows, blocks * FP8_BLOCK, dtype=_E4M3, device=device)
+    q.scales = torch.empty(blocks, rows, dtype=_U8, device=device)
+    return q
 
 
 class MoeOrder(NamedTuple):
@@ -701,23 +719,15 @@ class MoeOrder(NamedTuple):
     position: torch.Tensor
 
 
-def _require_int32(**named) -> None:
-    for name, t in named.items():
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-            raise TypeError(f"{name}: a contiguous int32 tensor")
-
-
-def _require_operand(q: Fp8, name: str) -> None:
-    (codes, scales) = q
-    if codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.uint8 or not codes.is_contiguous() or not scales.is_contiguous():
-        raise TypeError(f"{name}: contiguous float8_e4m3fn codes and uint8 scales")
-    if codes.dim() != 2 or codes.shape[1] % FP8_BLOCK or tuple(scales.shape) != (codes.shape[1] // FP8_BLOCK, codes.shape[0]):
-        raise ValueError(f"{name}: codes [rows, 128 S] with scales [S, rows]")
-
-
-def _fp8_empty(rows: int, blocks: int, like: torch.Tensor) -> Fp8:
-    return Fp8(torch.empty((rows, blocks * FP8_BLOCK), dtype=torch.float8_e4m3fn, device=like.device),
-               torch.empty((blocks, rows), dtype=torch.uint8, device=like.device))
+def _int32(t: torch.Tensor | None, name: str) -> int | None:
+    """The address of a contiguous int32 tensor on the GPU, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or not t.is_contiguous():
+        raise TypeError(f"{name}: a contiguous int32 tensor")
+    if not t.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    return t.data_ptr()
 
 
 def fp8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, order: torch.Tensor | None = None, top_k: int = 1,
@@ -725,144 +735,171 @@ def fp8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, order: 
     """nvfp4_fp8_quantize of x [R, C], or of a stack [E, R, C] of matrices (dense behind one another) -> (rows side, columns side),
     None for a side that is not wanted.  order (moe_sort's), top_k: row r is x[order[r] // top_k].  offsets (moe_sort's): column blocks
     start anew at each expert's first row."""
-    _require_gpu(x, order, offsets)
-    _require_int32(order=order, offsets=offsets)
-    if x.dim() not in (2, 3) or not (rows or cols) or (x.dim() == 3 and (order is not None or offsets is not None)):
-        raise ValueError("x: a matrix, or a stack of them without order and offsets; rows, cols or both")
-    if offsets is not None and not cols:
-        raise ValueError("offsets divide the columns' blocks: cols=True")
-    batch, (n, c) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
-    if c > 1 and x.stride(-1) != 1:
+    device = x.device
+    if device.type != "cuda":
+        raise ValueError("tensors must live on the GPU")
+    p_order, p_offsets = _int32(order, "order"), _int32(offsets, "offsets")
+    if x.dim() == 2:
+        batch, (n, c) = 1, x.shape
+        ld, lane = x.stride()
+        if n <= 1:
+            ld = c
+    elif x.dim() == 3 and order is None and offsets is None:
+        batch, n, c = x.shape
+        pitch, ld, lane = x.stride()
+        if n <= 1:
+            ld = pitch if batch > 1 else c
+        if batch > 1 and pitch != n * ld:
+            raise ValueError("x: matrices one behind the other")
+    else:
+        raise ValueError("x: a matrix, or a stack of them without order and offsets")
+    if lane != 1 and c > 1:
         raise ValueError("x: rows of neighbouring elements")
-    ld = x.stride(-2) if n > 1 else x.stride(0) if batch > 1 else c
-    if batch > 1 and x.stride(0) != n * ld:
-        raise ValueError("x: matrices one behind the other")
-    x_rows = n
+    if not rows and not cols or offsets is not None and not cols:
+        raise ValueError("rows, cols or both; offsets divide the columns' blocks")
+    x_rows, groups = n, 0
     if order is not None:
         n = order.numel()
-    groups = offsets.numel() - 1 if offsets is not None else 0
-    r = _fp8_empty(batch * n, -(-c // FP8_BLOCK), x) if rows else None
-    k = _fp8_empty(batch * c, n // FP8_BLOCK + groups if groups else -(-n // FP8_BLOCK), x) if cols else None
-    _check(lib.nvfp4_fp8_quantize(x.data_ptr(), _dtype_tag(x), batch, n, c, ld, order.data_ptr() if order is not None else None, top_k, x_rows,
-                                  offsets.data_ptr() if offsets is not None else None, groups,
-                                  r.codes.data_ptr() if rows else None, r.scales.data_ptr() if rows else None,
-                                  k.codes.data_ptr() if cols else None, k.scales.data_ptr() if cols else None, _stream()), "nvfp4_fp8_quantize")
+    if offsets is not None:
+        groups = offsets.numel() - 1
+    r = k = rc = rs = kc = ks = None
+    if rows:
+        r = _fp8_empty(batch * n, -(-c // FP8_BLOCK), device)
+        rc, rs = r.codes.data_ptr(), r.scales.data_ptr()
+    if cols:
+        k = _fp8_empty(batch * c, n // FP8_BLOCK + groups if groups else -(-n // FP8_BLOCK), device)
+        kc, ks = k.codes.data_ptr(), k.scales.data_ptr()
+    code = lib.nvfp4_fp8_quantize(x.data_ptr(), _dtype_tag(x), batch, n, c, ld, p_order, top_k, x_rows, p_offsets, groups, rc, rs, kc, ks, _stream())
+    if code:
+        _check(code, "nvfp4_fp8_quantize")
     return r, k
 
 
 def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """nvfp4_fp8_gemm: operands [M, K] and [N, K] -> [M, N]."""
-    _require_gpu(a.codes, a.scales, b.codes, b.scales, out)
-    _require_operand(a, "a")
-    _require_operand(b, "b")
     (M, K), (N, Kb) = a.codes.shape, b.codes.shape
     if K != Kb:
         raise ValueError(f"contractions of {K} and {Kb}")
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a.codes.device)
-    elif tuple(out.shape) != (M, N) or (N > 1 and out.stride(1) != 1):
-        raise ValueError(f"out: [{M}, {N}] in rows of neighbouring elements")
-    _check(lib.nvfp4_fp8_gemm(M, N, K, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), out.data_ptr(), _dtype_tag(out),
-                              out.stride(0) if M > 1 else N, _stream()), "nvfp4_fp8_gemm")
+        out, ldc = torch.empty(M, N, dtype=out_dtype, device=a.codes.device), N
+    else:
+        _require_gpu(out)
+        if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
+            raise ValueError(f"out: [{M}, {N}] in rows of neighbouring elements")
+        ldc = out.stride(0) if M > 1 else N
+    code = lib.nvfp4_fp8_gemm(M, N, K, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), out.data_ptr(), _dtype_tag(out), ldc,
+                              _stream())
+    if code:
+        _check(code, "nvfp4_fp8_gemm")
     return out
 
 
 def fp8_gemm_experts(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """nvfp4_fp8_gemm_experts: tokens in the experts' order [R, K] against their experts' rows of b [E * N, K] -> [R, N]."""
-    _require_gpu(a.codes, a.scales, b.codes, b.scales, offsets)
-    _require_operand(a, "a")
-    _require_operand(b, "b")
-    _require_int32(offsets=offsets)
-    (R, K), groups = a.codes.shape, offsets.numel() - 1
-    if groups < 1 or b.codes.shape[0] % groups or b.codes.shape[1] != K:
+    (R, K), (EN, Kb), p_offsets, groups = a.codes.shape, b.codes.shape, _int32(offsets, "offsets"), offsets.numel() - 1
+    if groups < 1 or EN % groups or Kb != K:
         raise ValueError(f"b: [{groups} experts * N, {K}]")
-    N = b.codes.shape[0] // groups
-    out = torch.empty((R, N), dtype=out_dtype, device=a.codes.device)
-    _check(lib.nvfp4_fp8_gemm_experts(R, N, K, groups, offsets.data_ptr(), a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(),
-                                      out.data_ptr(), _dtype_tag(out), N, _stream()), "nvfp4_fp8_gemm_experts")
+    N = EN // groups
+    out = torch.empty(R, N, dtype=out_dtype, device=a.codes.device)
+    code = lib.nvfp4_fp8_gemm_experts(R, N, K, groups, p_offsets, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(),
+                                      out.data_ptr(), _dtype_tag(out), N, _stream())
+    if code:
+        _check(code, "nvfp4_fp8_gemm_experts")
     return out
 
 
 def fp8_gemm_experts_dw(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16, rows: int | None = None) -> torch.Tensor:
     """nvfp4_fp8_gemm_experts_dw: columns operands [M, 128 S] and [N, 128 S] of two tensors with these offsets -> [E, M, N].
     rows: of these tensors (where left out, the most that S blocks can hold, which is as good)."""
-    _require_gpu(a.codes, a.scales, b.codes, b.scales, offsets)
-    _require_operand(a, "a")
-    _require_operand(b, "b")
-    _require_int32(offsets=offsets)
-    groups, slots = offsets.numel() - 1, a.scales.shape[0]
+    (M, width), (N, width_b), p_offsets, groups = a.codes.shape, b.codes.shape, _int32(offsets, "offsets"), offsets.numel() - 1
+    slots = width // FP8_BLOCK
     if rows is None:
         rows = (slots - groups) * FP8_BLOCK + FP8_BLOCK - 1
-    if groups < 1 or slots != rows // FP8_BLOCK + groups or b.scales.shape[0] != slots:
+    if groups < 1 or slots != rows // FP8_BLOCK + groups or width_b != width:
         raise ValueError(f"a, b: {rows // FP8_BLOCK + groups} blocks for {rows} rows of {groups} experts")
-    M, N = a.codes.shape[0], b.codes.shape[0]
-    out = torch.empty((groups, M, N), dtype=out_dtype, device=a.codes.device)
-    _check(lib.nvfp4_fp8_gemm_experts_dw(M, N, rows, groups, offsets.data_ptr(), a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
+    out = torch.empty(groups, M, N, dtype=out_dtype, device=a.codes.device)
+    _check(lib.nvfp4_fp8_gemm_experts_dw(M, N, rows, groups, p_offsets, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
                                          b.scales.data_ptr(), out.data_ptr(), _dtype_tag(out), N, _stream()), "nvfp4_fp8_gemm_experts_dw")
     return out
 
 
 def moe_sort(experts: torch.Tensor, groups: int) -> MoeOrder:
     """nvfp4_moe_sort: experts [T, top_k] (int32 or int64; numbers outside 0 .. groups - 1 drop the pair)."""
-    _require_gpu(experts)
-    if experts.dtype not in (torch.int32, torch.int64) or not experts.is_contiguous():
+    device, n, size = experts.device, experts.numel(), 8 if experts.dtype is torch.int64 else 4
+    if device.type != "cuda":
+        raise ValueError("tensors must live on the GPU")
+    if (size == 4 and experts.dtype is not _I32) or not experts.is_contiguous():
         raise TypeError("experts: a contiguous int32 or int64 tensor")
-    n, device = experts.numel(), experts.device
-    offsets = torch.empty(groups + 1 if groups > 0 else 1, dtype=torch.int32, device=device)
-    order = torch.empty(n, dtype=torch.int32, device=device)
-    position = torch.empty(experts.shape, dtype=torch.int32, device=device)
-    stream, ws_bytes = _stream(), lib.nvfp4_moe_sort_workspace_bytes(n, groups)
+    offsets = torch.empty(groups + 1 if groups > 0 else 1, dtype=_I32, device=device)
+    order = torch.empty(n, dtype=_I32, device=device)
+    position = torch.empty(*experts.shape, dtype=_I32, device=device) if experts.dim() else torch.empty((), dtype=_I32, device=device)
+    stream, key = _stream(), ("moe_sort", n, groups)
+    ws_bytes = _known_sizes.get(key)
+    if ws_bytes is None:
+        if len(_known_sizes) >= 1000:
+            _known_sizes.clear()
+        ws_bytes = _known_sizes[key] = lib.nvfp4_moe_sort_workspace_bytes(n, groups)
     block = _Block(ws_bytes, experts, stream) if ws_bytes else None
-    _check(lib.nvfp4_moe_sort(experts.data_ptr(), experts.element_size(), n, groups, offsets.data_ptr(), order.data_ptr(), position.data_ptr(),
-                              block.ptr if block else None, ws_bytes, stream), "nvfp4_moe_sort")
+    code = lib.nvfp4_moe_sort(experts.data_ptr(), size, n, groups, offsets.data_ptr(), order.data_ptr(), position.data_ptr(), block.ptr if block else None,
+                              ws_bytes, stream)
+    if code:
+        _check(code, "nvfp4_moe_sort")
     return MoeOrder(offsets, order, position)
 
 
 def moe_gather(x: torch.Tensor, order: torch.Tensor, top_k: int) -> torch.Tensor:
     """nvfp4_moe_gather: x [T, D] -> [pairs, D], row r = x[order[r] // top_k], zeros past the last kept pair."""
-    _require_gpu(x, order)
-    _require_int32(order=order)
+    _require_gpu(x)
+    p_order = _int32(order, "order")
     if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("x: a matrix in rows of neighbouring elements")
     (T, D), R = x.shape, order.numel()
-    out = torch.empty((R, D), dtype=x.dtype, device=x.device)
-    _check(lib.nvfp4_moe_gather(x.data_ptr(), _dtype_tag(x), T, D, x.stride(0) if T > 1 else D, order.data_ptr(), top_k, R, out.data_ptr(), _stream()),
-           "nvfp4_moe_gather")
+    out = torch.empty(R, D, dtype=x.dtype, device=x.device)
+    code = lib.nvfp4_moe_gather(x.data_ptr(), _dtype_tag(x), T, D, x.stride(0) if T > 1 else D, p_order, top_k, R, out.data_ptr(), _stream())
+    if code:
+        _check(code, "nvfp4_moe_gather")
     return out
 
 
-def _require_routing(position: torch.Tensor, weights: torch.Tensor | None) -> None:
-    _require_int32(position=position)
+def _routing(position: torch.Tensor, weights: torch.Tensor | None) -> tuple[int, int | None]:
+    p_position = _int32(position, "position")
     if position.dim() != 2 or position.shape[1] < 1:
         raise ValueError("position: [T, top_k]")
-    if weights is not None and (weights.dtype != torch.float32 or not weights.is_contiguous() or weights.shape != position.shape):
+    if weights is None:
+        return p_position, None
+    if weights.dtype is not torch.float32 or not weights.is_contiguous() or weights.shape != position.shape:
         raise TypeError("weights: a contiguous float32 tensor like position")
+    if not weights.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    return p_position, weights.data_ptr()
 
 
 def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None = None) -> torch.Tensor:
     """nvfp4_moe_combine: y [pairs, D], position [T, top_k] -> [T, D] = sum_j weights[t, j] y[position[t, j]]; without weights the plain sum,
     which is moe_gather's gradient."""
-    _require_gpu(y, position, weights)
-    _require_routing(position, weights)
+    _require_gpu(y)
+    p_position, p_weights = _routing(position, weights)
     if y.dim() != 2 or not y.is_contiguous():
         raise ValueError("y: a dense matrix")
     (R, D), (T, k) = y.shape, position.shape
-    out = torch.empty((T, D), dtype=y.dtype, device=y.device)
-    _check(lib.nvfp4_moe_combine(y.data_ptr(), _dtype_tag(y), R, D, weights.data_ptr() if weights is not None else None, position.data_ptr(), T, k,
-                                 out.data_ptr(), _stream()), "nvfp4_moe_combine")
+    out = torch.empty(T, D, dtype=y.dtype, device=y.device)
+    code = lib.nvfp4_moe_combine(y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, T, k, out.data_ptr(), _stream())
+    if code:
+        _check(code, "nvfp4_moe_combine")
     return out
 
 
 def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, weights: torch.Tensor, position: torch.Tensor,
                     offsets: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
     """nvfp4_moe_combine_bwd: the gradient of moe_combine(y, position, weights) for dout [T, D] -> (dy like y, dweights float32 like weights)."""
-    _require_gpu(dout, y, weights, position, offsets)
-    _require_routing(position, weights)
-    _require_int32(offsets=offsets)
-    if y.dim() != 2 or not y.is_contiguous() or not dout.is_contiguous() or dout.dtype != y.dtype or tuple(dout.shape) != (position.shape[0], y.shape[1]):
+    _require_gpu(dout, y)
+    p_offsets, (p_position, p_weights) = _int32(offsets, "offsets"), _routing(position, weights)
+    if y.dim() != 2 or not y.is_contiguous() or not dout.is_contiguous() or dout.dtype is not y.dtype or dout.shape != (position.shape[0], y.shape[1]):
         raise ValueError("y: a dense matrix; dout: dense [T, D] of its type")
     (R, D), (T, k) = y.shape, position.shape
     dy, dweights = torch.empty_like(y), torch.empty_like(weights)
-    _check(lib.nvfp4_moe_combine_bwd(dout.data_ptr(), y.data_ptr(), _dtype_tag(y), R, D, weights.data_ptr(), position.data_ptr(), offsets.data_ptr(),
-                                     offsets.numel() - 1, T, k, dy.data_ptr(), dweights.data_ptr(), _stream()), "nvfp4_moe_combine_bwd")
+    code = lib.nvfp4_moe_combine_bwd(dout.data_ptr(), y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, p_offsets, offsets.numel() - 1, T, k,
+                                     dy.data_ptr(), dweights.data_ptr(), _stream())
+    if code:
+        _check(code, "nvfp4_moe_combine_bwd")
     return dy, dweights

@@ -6,80 +6,98 @@
 
 namespace nvfp4 {
 
-// MT: fragments of 16 rows of A.  U: K tiles of a batch.
-template <int MODE, int OUT_DT, int MT, int U, int NW>
+// MT, TN: fragments of 16 rows of A and of 16 columns.  U: K tiles of a batch.
+template <int MODE, int OUT_DT, int MT, int TN, int U, int NW>
 __global__ __launch_bounds__(64 * NW) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
 {
     using namespace f8g;
-    __shared__ float4v_t sums[NW][MT][64];
+    __shared__ float4v_t sums[NW][MT * TN][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
-    const Tile T = find_tile<MODE>(P, blockIdx.x, 16 * MT, 16);
+    const Tile T = find_tile<MODE>(P, blockIdx.x, 16 * MT, 16 * TN);
     if (T.rows <= 0) return;
     const int64_t pitch = (int64_t)P.blocks * KT;
-    const int64_t brow = T.b0 + T.n0 + (c < T.cols ? c : T.cols - 1);
-    const uint8_t *const pb = P.B + brow * pitch + q * 16;
-    const uint8_t *pa[MT];
-    int64_t arow[MT];
+    // (rows past the edge repeat the last one)
+    const uint8_t *pb[TN], *psb[TN], *pa[MT], *psa[MT];
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+        const int r = 16 * b + c;
+        const int64_t row = T.b0 + T.n0 + (r < T.cols ? r : T.cols - 1);
+        pb[b] = P.B + row * pitch + q * 16;
+        psb[b] = P.B_scales + row;
+    }
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
         const int r = 16 * a + c;
-        arow[a] = T.m0 + (r < T.rows ? r : T.rows - 1);
-        pa[a] = P.A + arow[a] * pitch + q * 16;
+        const int64_t row = T.m0 + (r < T.rows ? r : T.rows - 1);
+        pa[a] = P.A + row * pitch + q * 16;
+        psa[a] = P.A_scales + row;
     }
-    float4v_t acc[MT];
+    float4v_t acc[MT][TN];
 #pragma unroll
-    for (int a = 0; a < MT; ++a) acc[a] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
     for (int kt = wave; kt < T.count; kt += NW * U) {
-        Codes fb[U], fa[U][MT];
-        uint32_t sb[U], sa[U][MT];
+        Codes fb[U][TN], fa[U][MT];
+        uint32_t sb[U][TN], sa[U][MT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             // (past the last K tile: the last once more, and not multiplied)
             const int64_t k = kt + u * NW < T.count ? kt + u * NW : T.count - 1;
-            fb[u].lo = *reinterpret_cast<const u32x4_t *>(pb + k * KT);
-            fb[u].hi = *reinterpret_cast<const u32x4_t *>(pb + k * KT + 64);
-            sb[u] = P.B_scales[k * P.b_rows + brow];
+#pragma unroll
+            for (int b = 0; b < TN; ++b) {
+                fb[u][b].lo = *reinterpret_cast<const u32x4_t *>(pb[b] + k * KT);
+                fb[u][b].hi = *reinterpret_cast<const u32x4_t *>(pb[b] + k * KT + 64);
+                sb[u][b] = psb[b][k * P.b_rows];
+            }
 #pragma unroll
             for (int a = 0; a < MT; ++a) {
                 fa[u][a].lo = *reinterpret_cast<const u32x4_t *>(pa[a] + k * KT);
                 fa[u][a].hi = *reinterpret_cast<const u32x4_t *>(pa[a] + k * KT + 64);
-                sa[u][a] = P.A_scales[k * P.a_rows + arow[a]];
+                sa[u][a] = psa[a][k * P.a_rows];
             }
         }
+        __builtin_amdgcn_sched_barrier(0);  // (all of a batch's loads first)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (kt + u * NW < T.count) {
                 if constexpr (OUT_DT == NVFP4_F32) {
-                    const Expanded b = expand(fb[u], sb[u]);
 #pragma unroll
-                    for (int a = 0; a < MT; ++a) multiply(acc[a], b, expand(fa[u][a], sa[u][a]));
+                    for (int b = 0; b < TN; ++b) {
+                        const Expanded eb = expand(fb[u][b], sb[u][b]);
+#pragma unroll
+                        for (int a = 0; a < MT; ++a) multiply(acc[a][b], eb, expand(fa[u][a], sa[u][a]));
+                    }
                 } else {
 #pragma unroll
-                    for (int a = 0; a < MT; ++a)
-                        acc[a] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u].all(), fa[u][a].all(), acc[a], 0, 0, 0, sb[u], 0, sa[u][a]);
+                    for (int b = 0; b < TN; ++b)
+#pragma unroll
+                        for (int a = 0; a < MT; ++a)
+                            acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][b].all(), fa[u][a].all(), acc[a][b], 0, 0, 0, sb[u][b], 0, sa[u][a]);
                 }
             }
         }
     }
 #pragma unroll
-    for (int a = 0; a < MT; ++a) sums[wave][a][lane] = acc[a];
-    __syncthreads();
-    // lane (c, q) of a wave: row c of fragment a, columns 4 q .. 4 q + 3
-    for (int a = wave; a < MT; a += NW) {
-        float4v_t s = sums[0][a][lane];
+    for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int w = 1; w < NW; ++w) s += sums[w][a][lane];
-        const int row = 16 * a + c, n = T.cols - 4 * q;
-        const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + 4 * q;
-        if (row < T.rows && n > 0) store_four<OUT_DT>(P.out, at, s, n);
+        for (int b = 0; b < TN; ++b) sums[wave][TN * a + b][lane] = acc[a][b];
+    __syncthreads();
+    // lane (c, q) of a wave: row c of fragment a, columns 4 q .. 4 q + 3 of fragment b
+    for (int f = wave; f < MT * TN; f += NW) {
+        float4v_t s = sums[0][f][lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) s += sums[w][f][lane];
+        const int row = 16 * (f / TN) + c, col = 16 * (f % TN) + 4 * q;
+        if (row < T.rows && col < T.cols) store_four<OUT_DT>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col, s, T.cols - col);
     }
 }
 
-template <int MODE, int MT, int U, int NW>
+template <int MODE, int MT, int TN, int U, int NW>
 static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
-    auto *k = out_dt == NVFP4_F32 ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, U, NW> : fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, U, NW>;
-    k<<<dim3((unsigned)f8g::tiles<MODE>(P, 16 * MT, 16)), 64 * NW, 0, st>>>(P);
+    auto *k = out_dt == NVFP4_F32 ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, TN, U, NW> : fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, TN, U, NW>;
+    k<<<dim3((unsigned)f8g::tiles<MODE>(P, 16 * MT, 16 * TN)), 64 * NW, 0, st>>>(P);
     return hipGetLastError();
 }
 
@@ -90,10 +108,9 @@ bool fp8_gemm_is_thin(const Fp8GemmArgs &P, int mode)
 
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
 {
-    if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, 1, 4, 8>(P, out_dt, st);
-    if (P.M <= 16) return launch_thin<FP8_DENSE, 1, 4, 8>(P, out_dt, st);
-    if (P.M <= 32) return launch_thin<FP8_DENSE, 2, 4, 8>(P, out_dt, st);
-    return launch_thin<FP8_DENSE, 4, 2, 8>(P, out_dt, st);
+    if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, 1, 2, 4, 4>(P, out_dt, st);
+    if (P.M > 16) return P.N <= 4096 ? launch_thin<FP8_DENSE, 2, 1, 4, 8>(P, out_dt, st) : P.N <= 8192 ? launch_thin<FP8_DENSE, 2, 2, 2, 8>(P, out_dt, st) : launch_thin<FP8_DENSE, 2, 3, 2, 8>(P, out_dt, st);
+    return P.N <= 4096 ? launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st) : P.N <= 8192 ? launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st) : launch_thin<FP8_DENSE, 1, 3, 4, 8>(P, out_dt, st);
 }
 
 }  // namespace nvfp4
