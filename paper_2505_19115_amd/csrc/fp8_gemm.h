@@ -168,6 +168,26 @@ __device__ __forceinline__ void store_four(void *out, int64_t at, const float4v_
     }
 }
 
+// n of eight columns of one row, in bf16, masked
+__device__ __forceinline__ void store_eight(void *out, int64_t at, const float (&v)[8], int n, uint32_t keep)
+{
+    struct __attribute__((packed, aligned(2))) P { u32x4_t w; };
+    uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
+    u32x4_t w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2v_t f = {v[2 * i], v[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t)) & keep;
+    }
+    if (n >= 8) {
+        reinterpret_cast<P *>(p)->w = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
 // Sixteen columns of one row from a lane's accumulators v[4 i + j] = column 4 i + j.  Rows of the output start at any element.
 template <int OUT_DT>
 __device__ __forceinline__ void store_sixteen(void *out, int64_t at, const float (&v)[16], int n)

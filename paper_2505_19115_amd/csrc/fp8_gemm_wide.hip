@@ -2,8 +2,10 @@
 // wave per SIMD).  A K tile is 64 MFMAs a wave, 32 cycles each, and 128 KB out of the LDS for the four of them, half of what it delivers
 // in that time.
 //
-// LDS: two stages of one K tile, 32 KB of each operand, placed as in fp8_gemm.hip (row 64 g + 4 c + j at position 64 g + 16 j + c, chunk h at slot h ^ (c / 2)), and
-// its 512 scale bytes, a dword each in the rows' order, so that a lane's four fragments' come in one read.  All of it is written by direct global ->
+// LDS: two stages of one K tile, 32 KB of each operand, 16 positions a fragment; chunk h of position 16 f + c at slot h ^ (c / 2), and lane (c, q) reads chunks
+// q and q + 4 (fp8_gemm.hip).  A's rows stand in their order; B's so that a lane ends with eight neighbouring columns and its three neighbours with those
+// beside them, one store of 64 bytes a row: fragment 2 s + h of 64 columns has the columns 32 s + 8 (c / 4) + 4 h + c % 4.  Beside them the 512 scale
+// bytes, a dword each, four fragments' of a lane together.  All of it is written by direct global ->
 // LDS loads (scales byte by byte: they start anywhere), so that the loads in flight can be counted.  Rows past the edge are clamped to the last one.
 //
 // A K tile in quarters, halves of A against halves of B, a half's registers read again as soon as its last quarter is done; of B the half that
@@ -14,6 +16,11 @@
 // scales in a tile's first quarter, Q and A1 in its third.  So a load has a K tile and a quarter at least; with the loads behind the first barrier only,
 // three quarters, 4096 x 4096 x 11008 took 167 us.  Past the last K tile the loads repeat one piece of the first, so that
 // the counts hold.
+//
+// Workgroups stay (one per CU) and walk the output tiles: the first two K tiles of the next one are requested before this one's outputs are
+// stored.  Which tiles there are for how many rows of an expert is
+// counted once, into the LDS.
+#include <atomic>
 #include <type_traits>
 
 #include "fp8_gemm.h"
@@ -22,8 +29,12 @@ namespace nvfp4 {
 namespace f8w {
 
 constexpr int BM = 256, BN = 256, KT = FP8_BLOCK;
-constexpr int STAGE = (BM + BN) * KT, SCALES = (BM + BN) * 4, SCALES0 = 2 * STAGE, LDS_BYTES = SCALES0 + 2 * SCALES;
+constexpr int STAGE = (BM + BN) * KT, SCALES = (BM + BN) * 4, SCALES0 = 2 * STAGE, GROUPS0 = SCALES0 + 2 * SCALES;
+constexpr int LDS_BYTES = GROUPS0 + 2 * 4 * (MAX_EXPERTS + 2);
 constexpr int FIRST = 10, SECOND = 8;  // loads of a wave and K tile: A0, P and scales; Q and A1
+
+// Column (of 64) that position c of fragment f holds
+__device__ __forceinline__ int column(int f, int c) { return 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3); }
 
 // As assembly, so that the 64 accumulators stay where they are (gemm_mx.hip).  What the compiler does not know about it: an operand must not have been
 // written by the vector ALU in the two instructions before (they come from LDS reads), and the last result must not be read for 11 wait
@@ -62,35 +73,123 @@ template <int MODE>
 __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 {
     using namespace f8g;
-    constexpr int BM = f8w::BM, BN = f8w::BN, STAGE = f8w::STAGE;
+    constexpr int BM = f8w::BM, BN = f8w::BN, STAGE = f8w::STAGE, ALL = f8w::FIRST + f8w::SECOND;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
     const int wm = wave >> 1, wn = wave & 1;
-    const Tile T = find_tile<MODE>(P, blockIdx.x, BM, BN);
-    if (T.rows <= 0) return;
     const int64_t pitch = (int64_t)P.blocks * KT;
+
+    // ---- which tiles there are.  Groups' first rows (clamped, ascending) and, for the experts' product, their first tile rows, with the rows of no expert
+    // as one more group.
+    const int ntx = (int)((P.N + BN - 1) / BN);
+    int *const group_row = reinterpret_cast<int *>(lds + f8w::GROUPS0), *const group_tile = group_row + MAX_EXPERTS + 2;
+    int nty = (int)((P.M + BM - 1) / BM);
+    if (MODE != FP8_DENSE) {
+        const int total = MODE == FP8_EXPERTS ? (int)P.M : P.total, groups = P.groups + (MODE == FP8_EXPERTS ? 1 : 0);
+        if (wave == 0) {
+            int row = 0, tiles = 0;
+            for (int e0 = 0; e0 <= groups; e0 += 64) {
+                // (an offset below an earlier one counts as that one, so that groups do not overlap)
+                const int e = e0 + lane;
+                int a = e <= P.groups ? P.offsets[e] : total;
+                a = a < 0 ? 0 : a > total ? total : a;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int up = __shfl_up(a, d);
+                    if (lane >= d) a = a > up ? a : up;
+                }
+                a = a > row ? a : row;
+                if (e <= groups) group_row[e] = a;
+                if (MODE == FP8_EXPERTS) {
+                    // tiles of the group before, which ends here
+                    int before = __shfl_up(a, 1);
+                    before = lane == 0 ? row : before;
+                    int n = e == 0 || e > groups ? 0 : (a - before + BM - 1) / BM;
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) {
+                        const int up = __shfl_up(n, d);
+                        if (lane >= d) n += up;
+                    }
+                    if (e <= groups) group_tile[e] = tiles + n;
+                    tiles += __shfl(n, 63);
+                }
+                row = __shfl(a, 63);
+            }
+        }
+        __syncthreads();
+        nty = MODE == FP8_EXPERTS ? __builtin_amdgcn_readfirstlane(group_tile[groups]) : nty * P.groups;
+    }
+    // An output without a contraction (rows of no expert, an expert without rows) is one K tile of whatever is there, stored as zeros: `keep` is a mask.
+    auto find = [&](int id, uint32_t &keep) -> Tile {
+        Tile T;
+        keep = ~0u;
+        int ty, tx;
+        tile_coords(id, ntx, nty, ty, tx);
+        T.k0 = 0;
+        T.count = P.blocks;
+        T.b0 = T.out = 0;
+        int left;
+        if constexpr (MODE == FP8_EXPERTS) {
+            int n = 0;
+            for (int e0 = 0; e0 <= P.groups; e0 += 64) n += __popcll(__ballot(e0 + lane <= P.groups && group_tile[e0 + lane <= P.groups ? e0 + lane : 0] <= ty));
+            const int e = __builtin_amdgcn_readfirstlane(n - 1);
+            const int row = __builtin_amdgcn_readfirstlane(group_row[e] + (ty - group_tile[e]) * BM), end = __builtin_amdgcn_readfirstlane(group_row[e + 1]);
+            T.m0 = row;
+            left = end - row;
+            if (e < P.groups) T.b0 = e * P.N;
+            else keep = 0;  // rows of no expert: zeros
+        } else {
+            if (MODE == FP8_EXPERTS_DW) {
+                const int per = nty / P.groups, e = ty / per;
+                ty -= e * per;
+                const int row = __builtin_amdgcn_readfirstlane(group_row[e]), rows = __builtin_amdgcn_readfirstlane(group_row[e + 1]) - row;
+                T.k0 = row / KT + e;
+                T.count = rows > 0 ? (rows + KT - 1) / KT : 1;
+                keep = rows > 0 ? ~0u : 0u;
+                T.out = e * P.M;
+            }
+            T.m0 = (int64_t)ty * BM;
+            left = P.M - T.m0 < BM ? (int)(P.M - T.m0) : BM;
+        }
+        T.n0 = (int64_t)tx * BN;
+        T.rows = left < BM ? left : BM;
+        T.cols = (int)(P.N - T.n0 < BN ? P.N - T.n0 : BN);
+        return T;
+    };
 
     // ---- global -> LDS: instruction u of four of a half fills 8 of the wave's 32 positions of it.  (Half h: positions 64 h .. + 63 of
     // each 128.)
-    uint32_t offA[8], offB[8];  // [half][u]
+    uint32_t offA[8], offB[8], offSA, offSB;  // [half][u]
     const int first = 128 * (wave >> 1), second = 32 * (wave & 1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int in = second + 8 * (i & 3) + (lane >> 3), at = in & 15, row = first + 64 * (i >> 2) + 4 * at + (in >> 4), chunk = (lane & 7) ^ (at >> 1);
-        offA[i] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + chunk * 16;
-        offB[i] = (uint32_t)((row < T.cols ? row : T.cols - 1) * pitch) + chunk * 16;
-    }
-    const int srow = wave * 64 + lane;
-    uint32_t offSA = srow < T.rows ? srow : T.rows - 1, offSB = srow < T.cols ? srow : T.cols - 1;
+    // K tile that is requested next
+    const uint8_t *pA, *pB, *pSA, *pSB;
+    int64_t step, stepSA, stepSB;
     auto uniform = [](const uint8_t *p) -> const uint8_t * {
         const uint64_t v = reinterpret_cast<uint64_t>(p);
         const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
         return reinterpret_cast<const uint8_t *>(((uint64_t)hi << 32) | lo);
     };
-    // K tile that is requested next
-    const uint8_t *pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT), *pB = uniform(P.B + (T.b0 + T.n0) * pitch + (int64_t)T.k0 * KT);
-    const uint8_t *pSA = uniform(P.A_scales + T.k0 * P.a_rows + T.m0), *pSB = uniform(P.B_scales + T.k0 * P.b_rows + T.b0 + T.n0);
-    int64_t step = KT, stepSA = P.a_rows, stepSB = P.b_rows;
+    auto point_to = [&](const Tile &T) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int in = second + 8 * (i & 3) + (lane >> 3), chunk = (lane & 7) ^ ((in & 15) >> 1), row = first + 64 * (i >> 2) + in,
+                      col = first + 64 * (i >> 2) + f8w::column(in >> 4, in & 15);
+            offA[i] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + chunk * 16;
+            offB[i] = (uint32_t)((col < T.cols ? col : T.cols - 1) * pitch) + chunk * 16;
+        }
+        // dword 4 c + f of the wave's 64: fragment f's position c
+        const int row = wave * 64 + 16 * (lane & 3) + (lane >> 2), col = wave * 64 + f8w::column(lane & 3, lane >> 2);
+        offSA = row < T.rows ? row : T.rows - 1;
+        offSB = col < T.cols ? col : T.cols - 1;
+        pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT);
+        pB = uniform(P.B + (T.b0 + T.n0) * pitch + (int64_t)T.k0 * KT);
+        pSA = uniform(P.A_scales + T.k0 * P.a_rows + T.m0);
+        pSB = uniform(P.B_scales + T.k0 * P.b_rows + T.b0 + T.n0);
+        step = KT;
+        stepSA = P.a_rows;
+        stepSB = P.b_rows;
+        asm volatile("s_nop 4");  // (a lane read's register as an address, five wait states later)
+    };
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds, dst = __builtin_amdgcn_readfirstlane(lds0 + (first + second) * KT),
                    dstS = __builtin_amdgcn_readfirstlane(lds0 + f8w::SCALES0 + wave * 256);
@@ -123,6 +222,19 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         pSB = P.B_scales;
         step = stepSA = stepSB = 0;
     };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    // K tiles 0 and 1 of an output tile
+    auto request_start = [&](const Tile &T) {
+        point_to(T);
+        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I0{}, i); });
+        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I0{}, i); });
+        advance();
+        if (T.count < 2) past_end();
+        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I1{}, i); });
+        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I1{}, i); });
+        advance();
+    };
 
     // ---- LDS -> registers: fragment f of the wave's 128 rows of an operand
     const int s0 = (q ^ (c >> 1)) << 4;
@@ -138,38 +250,83 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             baseA[s][h] = (const uint8_t *)(lds_ptr_t)(uintptr_t)v;
             baseB[s][h] = (const uint8_t *)(lds_ptr_t)(uintptr_t)w;
         }
-    Codes A[8], B[8];
-    auto read_a = [&](int st, int f, int h) { (h ? A[f].hi : A[f].lo) = *reinterpret_cast<const u32x4_t *>(baseA[st][h] + 16 * f * KT); };
-    auto read_b = [&](int st, int f, int h) { (h ? B[f].hi : B[f].lo) = *reinterpret_cast<const u32x4_t *>(baseB[st][h] + 16 * f * KT); };
-
-    float4v_t acc[8][8];
-#pragma unroll
-    for (int a = 0; a < 8; ++a)
-#pragma unroll
-        for (int b = 0; b < 8; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-    // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
-    u32x4_t SA[2][2], SB[2][2];
     const uint8_t *baseSA = lds + f8w::SCALES0 + (wm * 128 + 4 * c) * 4, *baseSB = lds + f8w::SCALES0 + (BM + wn * 128 + 4 * c) * 4;
-    auto read_scales = [&](int st, int i) {
-        (i < 2 ? SA[st][i & 1] : SB[st][i & 1]) = *reinterpret_cast<const u32x4_t *>((i < 2 ? baseSA : baseSB) + st * f8w::SCALES + (i & 1) * 256);
-    };
-    // everything but the last n loads has landed and all of the wave's LDS reads are done; then the same of every wave
-#define NVFP4_F8W_BARRIER(n)                                                    \
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(n) : "memory"); \
-    __builtin_amdgcn_s_barrier();                                               \
+    // everything but the last n loads (and stores) has landed and all of the wave's LDS reads are done; then the same of every wave
+#define NVFP4_F8W_WAIT(n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(n) : "memory");
+#define NVFP4_F8W_BARRIER               \
+    __builtin_amdgcn_s_barrier(); \
     asm volatile("" ::: "memory");
-    using I0 = std::integral_constant<int, 0>;
-    using I1 = std::integral_constant<int, 1>;
-    if (T.count > 0) {
-        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I0{}, i); });
-        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I0{}, i); });
-        advance();
-        if (T.count < 2) past_end();
-        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I1{}, i); });
-        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I1{}, i); });
-        advance();
-        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
+
+    const int tiles = ntx * nty;
+    int id = (int)blockIdx.x;
+    if (id >= tiles) return;
+    uint32_t keep, next_keep = 0;
+    Tile T = find(id, keep);
+    request_start(T);
+    NVFP4_F8W_WAIT(ALL)
+    while (true) {
+        // here: K tile 0 has landed, as far as this wave is concerned
+        float4v_t acc[8][8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+#pragma unroll
+            for (int b = 0; b < 8; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+        Codes A[8], B[8];
+        auto read_a = [&](int st, int f, int h) { (h ? A[f].hi : A[f].lo) = *reinterpret_cast<const u32x4_t *>(baseA[st][h] + 16 * f * KT); };
+        auto read_b = [&](int st, int f, int h) { (h ? B[f].hi : B[f].lo) = *reinterpret_cast<const u32x4_t *>(baseB[st][h] + 16 * f * KT); };
+        // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
+        u32x4_t SA[2][2], SB[2][2];
+        auto read_scales = [&](int st, int i) {
+            (i < 2 ? SA[st][i & 1] : SB[st][i & 1]) = *reinterpret_cast<const u32x4_t *>((i < 2 ? baseSA : baseSB) + st * f8w::SCALES + (i & 1) * 256);
+        };
+            int kt = 0;
+        // stage ST, which is also the half P of B
+        auto tile = [&](auto stage) {
+            constexpr int ST = decltype(stage)::value;
+            using HP = std::integral_constant<int, ST>;
+            using HQ = std::integral_constant<int, 1 - ST>;
+            if (kt + 2 >= T.count) past_end();
+            asm volatile("s_nop 1");  // (accumulators that were just cleared: two instructions between that and the MFMAs)
+            __builtin_amdgcn_sched_barrier(0);
+            // MFMA j of a quarter: along a row of tiles and back along the next, one operand changes at a time
+            auto quarter = [&](auto ha, auto hb, auto &&between) {
+                f8w::each<0, 16>([&](auto j) {
+                    constexpr int J = decltype(j)::value, r = J >> 2, i = r & 1 ? 3 - (J & 3) : J & 3;
+                    constexpr int a = 4 * decltype(ha)::value + r, b = 4 * decltype(hb)::value + i;
+                    f8w::mfma(acc[a][b], B[b].all(), A[a].all(), SB[ST][b >> 2][b & 3], SA[ST][a >> 2][a & 3]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    between(j);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            };
+            quarter(I0{}, HP{}, [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if constexpr (J < 8) read_b(ST, 4 * (1 - ST) + (J >> 1), J & 1);
+                if constexpr (J >= 16 - f8w::FIRST) request_first(stage, std::integral_constant<int, J - (16 - f8w::FIRST)>{});
+            });
+            quarter(I0{}, HQ{}, [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if constexpr (J < 8) read_a(ST, 4 + (J >> 1), J & 1);
+            });
+            NVFP4_F8W_WAIT(ALL)
+            NVFP4_F8W_BARRIER
+            __builtin_amdgcn_sched_barrier(0);
+            quarter(I1{}, HQ{}, [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if constexpr (J < 8) read_a(1 - ST, J >> 1, J & 1);
+                if constexpr (J >= 8) request_second(stage, std::integral_constant<int, J - 8>{});
+            });
+            advance();
+            quarter(I1{}, HP{}, [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if constexpr (J < 8) read_b(1 - ST, 4 * (1 - ST) + (J >> 1), J & 1);
+                if constexpr (J >= 8 && J < 12) read_scales(1 - ST, J - 8);
+            });
+            NVFP4_F8W_WAIT(ALL)
+            NVFP4_F8W_BARRIER
+            ++kt;
+        };
+        NVFP4_F8W_BARRIER
 #pragma unroll
         for (int f = 0; f < 4; ++f)
 #pragma unroll
@@ -180,77 +337,64 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
         for (int i = 0; i < 4; ++i) read_scales(0, i);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    }
-    int kt = 0;
-    // stage ST, which is also the half P of B
-    auto tile = [&](auto stage) {
-        constexpr int ST = decltype(stage)::value;
-        using HP = std::integral_constant<int, ST>;
-        using HQ = std::integral_constant<int, 1 - ST>;
-        if (kt + 2 >= T.count) past_end();
-        __builtin_amdgcn_sched_barrier(0);
-        // MFMA j of a quarter: along a row of tiles and back along the next, one operand changes at a time
-        auto quarter = [&](auto ha, auto hb, auto &&between) {
-            f8w::each<0, 16>([&](auto j) {
-                constexpr int J = decltype(j)::value, r = J >> 2, i = r & 1 ? 3 - (J & 3) : J & 3;
-                constexpr int a = 4 * decltype(ha)::value + r, b = 4 * decltype(hb)::value + i;
-                f8w::mfma(acc[a][b], B[b].all(), A[a].all(), SB[ST][b >> 2][b & 3], SA[ST][a >> 2][a & 3]);
-                __builtin_amdgcn_sched_barrier(0);
-                between(j);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-        };
-        quarter(I0{}, HP{}, [&](auto j) {
-            constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_b(ST, 4 * (1 - ST) + (J >> 1), J & 1);
-            if constexpr (J >= 16 - f8w::FIRST) request_first(stage, std::integral_constant<int, J - (16 - f8w::FIRST)>{});
-        });
-        quarter(I0{}, HQ{}, [&](auto j) {
-            constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_a(ST, 4 + (J >> 1), J & 1);
-        });
-        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
-        __builtin_amdgcn_sched_barrier(0);
-        quarter(I1{}, HQ{}, [&](auto j) {
-            constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_a(1 - ST, J >> 1, J & 1);
-            if constexpr (J >= 8) request_second(stage, std::integral_constant<int, J - 8>{});
-        });
-        advance();
-        quarter(I1{}, HP{}, [&](auto j) {
-            constexpr int J = decltype(j)::value;
-            if constexpr (J < 8) read_b(1 - ST, 4 * (1 - ST) + (J >> 1), J & 1);
-            if constexpr (J >= 8 && J < 12) read_scales(1 - ST, J - 8);
-        });
-        NVFP4_F8W_BARRIER(f8w::FIRST + f8w::SECOND)
-        ++kt;
-    };
-    while (kt + 2 <= T.count) {
-        tile(I0{});
-        tile(I1{});
-    }
-    if (kt < T.count) tile(I0{});
-#undef NVFP4_F8W_BARRIER
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the loads past the end, before the workgroup's LDS is another's)
-    asm volatile("s_nop 15" ::: "memory");
-#pragma unroll
-    for (int a = 0; a < 8; ++a)
-#pragma unroll
-        for (int b = 0; b < 8; ++b) asm volatile("" : "+a"(acc[a][b]));
-#pragma unroll
-    for (int a = 0; a < 8; ++a)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int row = wm * 128 + 64 * (a >> 2) + 4 * c + (a & 3), col = wn * 128 + 64 * g + 16 * q;
-            float v[16];
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[4 * i + b] = acc[a][4 * g + b][i];
-            if (row < T.rows && col < T.cols) store_sixteen<NVFP4_BF16>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col, v, T.cols - col);
+        NVFP4_F8W_BARRIER
+        while (kt + 2 <= T.count) {
+            tile(I0{});
+            tile(I1{});
         }
+        if (kt < T.count) tile(I0{});
+        // Every wave has read all that it needed: the next tile's loads may follow (behind this one's past its end, to the same places, of which each
+        // has one wave that loads it).
+        id += (int)gridDim.x;
+        Tile next = T;
+        if (id < tiles) {
+            next = find(id, next_keep);
+            request_start(next);
+        }
+        asm volatile("s_nop 15" ::: "memory");
+        // The next tile's first K tile has landed when its second and what was stored behind that (32 stores inside the output, as few as none at its
+        // edge) are all that is outstanding.
+        auto store = [&](auto inside) {
+            int at_lane = lane;
+            asm volatile("" : "+v"(at_lane));  // (or the addresses are computed before the K loop and kept)
+            const int c = at_lane & 15, q = at_lane >> 4;
+#pragma unroll
+            for (int a = 0; a < 8; ++a)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int row = wm * 128 + 16 * a + c, col = wn * 128 + 32 * s + 8 * q;
+                    float v[8];
+                    // (reads that stay behind the wait states and leave the accumulators alone)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
+                    const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + col;
+                    if constexpr (decltype(inside)::value != 0) store_eight(P.out, at, v, 8, keep);
+                    else if (row < T.rows && col < T.cols) store_eight(P.out, at, v, T.cols - col, keep);
+                }
+            NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? 32 : 0))
+        };
+        if (T.rows == BM && T.cols == BN) store(I1{});
+        else store(I0{});
+        if (id >= tiles) break;
+        T = next;
+        keep = next_keep;
+    }
+#undef NVFP4_F8W_BARRIER
+#undef NVFP4_F8W_WAIT
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the loads past the end, before the workgroup's LDS is another's)
+}
+
+// Of the current device; a multiple of 8, so that a workgroup's tiles stay on its XCD's part of the walk
+static int64_t compute_units()
+{
+    static std::atomic<int> known[64];
+    int device = 0, n = 0;
+    if (hipGetDevice(&device) != hipSuccess) return 256;
+    if (device >= 0 && device < 64 && (n = known[device].load(std::memory_order_relaxed)) != 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n < 8) n = 256;
+    n = n / 8 * 8;
+    if (device >= 0 && device < 64) known[device].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 template <int MODE>
@@ -259,12 +403,14 @@ static hipError_t launch_wide(const Fp8GemmArgs &P, hipStream_t st)
     auto *k = fp8_gemm_wide_kernel<MODE>;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, f8w::LDS_BYTES);
     if (once != hipSuccess) return once;
-    k<<<dim3((unsigned)f8g::tiles<MODE>(P, f8w::BM, f8w::BN)), 256, f8w::LDS_BYTES, st>>>(P);
+    const int64_t tiles = f8g::tiles<MODE>(P, f8w::BM, f8w::BN), cus = compute_units();
+    k<<<dim3((unsigned)(tiles < cus ? tiles : cus)), 256, f8w::LDS_BYTES, st>>>(P);
     return hipGetLastError();
 }
 
 bool fp8_gemm_is_wide(const Fp8GemmArgs &P, int mode)
 {
+    if (P.blocks == 0) return false;
     const int64_t ntx = (P.N + 255) / 256;
     if (mode == FP8_DENSE) return ntx * ((P.M + 255) / 256) >= 128;
     if (mode == FP8_EXPERTS) return ntx * (P.M / 256) >= 128 && P.M >= 128 * (int64_t)P.groups;
