@@ -70,11 +70,15 @@ struct Fp8GemmArgs {
     int64_t ldc;
     const int32_t *offsets;
     int32_t groups, total;                // total (FP8_EXPERTS_DW): the rows that the offsets divide
+    int32_t stream;                       // the output leaves by nontemporal stores (set by launch_fp8_gemm())
 };
-bool fp8_gemm_is_thin(const Fp8GemmArgs &P, int mode);  // few rows: of all, or of each expert on average
+// The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
+// few tiles; 256 rows by 128 to 256 columns, bf16 outputs; 128 x 128.
+double fp8_gemm_thin_cost(const Fp8GemmArgs &P, int mode);
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
-bool fp8_gemm_is_wide(const Fp8GemmArgs &P, int mode);  // bf16 outputs on 256 x 256 tiles
+double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode);
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, hipStream_t st);
+int64_t compute_units();
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 
 // Routing

@@ -169,9 +169,10 @@ __device__ __forceinline__ void store_four(void *out, int64_t at, const float4v_
 }
 
 // n of eight columns of one row, in bf16, masked
+template <bool STREAMED>
 __device__ __forceinline__ void store_eight(void *out, int64_t at, const float (&v)[8], int n, uint32_t keep)
 {
-    struct __attribute__((packed, aligned(2))) P { u32x4_t w; };
+    typedef u32x4_t __attribute__((aligned(2))) anywhere_t;
     uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
     u32x4_t w;
 #pragma unroll
@@ -180,7 +181,8 @@ __device__ __forceinline__ void store_eight(void *out, int64_t at, const float (
         w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t)) & keep;
     }
     if (n >= 8) {
-        reinterpret_cast<P *>(p)->w = w;
+        if (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<anywhere_t *>(p));
+        else *reinterpret_cast<anywhere_t *>(p) = w;
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)

@@ -101,16 +101,62 @@ static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
     return hipGetLastError();
 }
 
-bool fp8_gemm_is_thin(const Fp8GemmArgs &P, int mode)
+// Shapes of a workgroup's output: rows and columns in 16s.  What bounds these kernels is what a CU's loads bring, (MT + TN) * 16 rows of a K tile at 36 GB/s: the
+// fewest rounds of the CUs times that.
+namespace f8t {
+struct Shape {
+    int mt, tn;
+};
+constexpr Shape SHAPES[] = {{1, 1}, {1, 2}, {1, 3}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {4, 2}, {4, 3}, {4, 4}};
+constexpr double PER_16_ROWS = 0.057;  // us
+
+inline int64_t workgroups(const Fp8GemmArgs &P, int mode, Shape s)
 {
-    return mode == FP8_DENSE ? P.M <= 64 : P.M <= 16 * (int64_t)P.groups;
+    const int64_t rows = mode == FP8_EXPERTS ? (P.M < P.groups ? P.M : P.groups) + P.M / (16 * s.mt) : (P.M + 16 * s.mt - 1) / (16 * s.mt);
+    return rows * ((P.N + 16 * s.tn - 1) / (16 * s.tn));
+}
+}  // namespace f8t
+
+static f8t::Shape shape_of(const Fp8GemmArgs &P, int mode, double *cost)
+{
+    const int64_t cus = compute_units();
+    f8t::Shape best = f8t::SHAPES[0];
+    *cost = 1e30;
+    for (const f8t::Shape s : f8t::SHAPES) {
+        if (mode == FP8_EXPERTS && s.mt > 1) continue;
+        const double c = (double)((f8t::workgroups(P, mode, s) + cus - 1) / cus) * (s.mt + s.tn) * f8t::PER_16_ROWS;
+        if (c < *cost) {
+            *cost = c;
+            best = s;
+        }
+    }
+    return best;
+}
+
+double fp8_gemm_thin_cost(const Fp8GemmArgs &P, int mode)
+{
+    double cost;
+    shape_of(P, mode, &cost);
+    return cost;
 }
 
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
 {
     if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, 1, 2, 4, 4>(P, out_dt, st);
-    if (P.M > 16) return P.N <= 4096 ? launch_thin<FP8_DENSE, 2, 1, 4, 8>(P, out_dt, st) : P.N <= 8192 ? launch_thin<FP8_DENSE, 2, 2, 2, 8>(P, out_dt, st) : launch_thin<FP8_DENSE, 2, 3, 2, 8>(P, out_dt, st);
-    return P.N <= 4096 ? launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st) : P.N <= 8192 ? launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st) : launch_thin<FP8_DENSE, 1, 3, 4, 8>(P, out_dt, st);
+    double cost;
+    const f8t::Shape s = shape_of(P, mode, &cost);
+    switch (4 * s.mt + s.tn) {
+    case 5: return launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st);
+    case 6: return launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st);
+    case 7: return launch_thin<FP8_DENSE, 1, 3, 4, 8>(P, out_dt, st);
+    case 9: return launch_thin<FP8_DENSE, 2, 1, 4, 8>(P, out_dt, st);
+    case 10: return launch_thin<FP8_DENSE, 2, 2, 2, 8>(P, out_dt, st);
+    case 11: return launch_thin<FP8_DENSE, 2, 3, 2, 8>(P, out_dt, st);
+    case 12: return launch_thin<FP8_DENSE, 2, 4, 2, 8>(P, out_dt, st);
+    case 18: return launch_thin<FP8_DENSE, 4, 2, 2, 8>(P, out_dt, st);
+    case 19: return launch_thin<FP8_DENSE, 4, 3, 1, 8>(P, out_dt, st);
+    default: return launch_thin<FP8_DENSE, 4, 4, 1, 8>(P, out_dt, st);
+    }
 }
 
 }  // namespace nvfp4

@@ -28,12 +28,18 @@
 namespace nvfp4 {
 namespace f8w {
 
-constexpr int BM = 256, BN = 256, KT = FP8_BLOCK;
-constexpr int STAGE = (BM + BN) * KT, SCALES = (BM + BN) * 4, SCALES0 = 2 * STAGE, GROUPS0 = SCALES0 + 2 * SCALES;
-constexpr int LDS_BYTES = GROUPS0 + 2 * 4 * (MAX_EXPERTS + 2);
-constexpr int FIRST = 10, SECOND = 8;  // loads of a wave and K tile: A0, P and scales; Q and A1
+constexpr int BM = 256, KT = FP8_BLOCK;
+// FB: fragments of 16 columns of a wave; the workgroup's tile is 256 x 32 FB
+template <int FB>
+struct Geom {
+    static constexpr int BN = 32 * FB, HB = FB / 2;                     // fragments of a half of B
+    static constexpr int STAGE = (BM + BN) * KT, SCALES = 4 * 512;     // of a K tile; scale bytes: a dword for each of 8 fragments a wave
+    static constexpr int SCALES0 = 2 * STAGE, GROUPS0 = SCALES0 + 2 * SCALES, LDS_BYTES = GROUPS0 + 2 * 4 * (MAX_EXPERTS + 2);
+    static constexpr int FIRST = 4 + HB + 2, SECOND = HB + 4;           // loads of a wave and K tile: A0, P and scales; Q and A1
+    static constexpr int STORES = 4 * FB;                               // of a wave, for an output inside
+};
 
-// Column (of 64) that position c of fragment f holds
+// Column (of the wave's) that position c of fragment f holds
 __device__ __forceinline__ int column(int f, int c) { return 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3); }
 
 // As assembly, so that the 64 accumulators stay where they are (gemm_mx.hip).  What the compiler does not know about it: an operand must not have been
@@ -69,11 +75,12 @@ __device__ __forceinline__ void each(F &&f)
 
 }  // namespace f8w
 
-template <int MODE>
+template <int MODE, int FB>
 __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 {
     using namespace f8g;
-    constexpr int BM = f8w::BM, BN = f8w::BN, STAGE = f8w::STAGE, ALL = f8w::FIRST + f8w::SECOND;
+    using G = f8w::Geom<FB>;
+    constexpr int BM = f8w::BM, BN = G::BN, HB = G::HB, STAGE = G::STAGE, ALL = G::FIRST + G::SECOND;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
     const int wm = wave >> 1, wn = wave & 1;
@@ -82,7 +89,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     // ---- which tiles there are.  Groups' first rows (clamped, ascending) and, for the experts' product, their first tile rows, with the rows of no expert
     // as one more group.
     const int ntx = (int)((P.N + BN - 1) / BN);
-    int *const group_row = reinterpret_cast<int *>(lds + f8w::GROUPS0), *const group_tile = group_row + MAX_EXPERTS + 2;
+    int *const group_row = reinterpret_cast<int *>(lds + G::GROUPS0), *const group_tile = group_row + MAX_EXPERTS + 2;
     int nty = (int)((P.M + BM - 1) / BM);
     if (MODE != FP8_DENSE) {
         const int total = MODE == FP8_EXPERTS ? (int)P.M : P.total, groups = P.groups + (MODE == FP8_EXPERTS ? 1 : 0);
@@ -157,10 +164,10 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         return T;
     };
 
-    // ---- global -> LDS: instruction u of four of a half fills 8 of the wave's 32 positions of it.  (Half h: positions 64 h .. + 63 of
-    // each 128.)
-    uint32_t offA[8], offB[8], offSA, offSB;  // [half][u]
-    const int first = 128 * (wave >> 1), second = 32 * (wave & 1);
+    // ---- global -> LDS.  Half h of A is positions 64 h .. + 63 of each 128, of B 16 HB h .. of each 16 FB; a wave's instructions fill 8
+    // positions each, half of one of the two parts.
+    uint32_t offA[8], offB[FB], offSA, offSB;  // [half][instruction]
+    const int part = wave >> 1, side = wave & 1;
     // K tile that is requested next
     const uint8_t *pA, *pB, *pSA, *pSB;
     int64_t step, stepSA, stepSB;
@@ -172,13 +179,16 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     auto point_to = [&](const Tile &T) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int in = second + 8 * (i & 3) + (lane >> 3), chunk = (lane & 7) ^ ((in & 15) >> 1), row = first + 64 * (i >> 2) + in,
-                      col = first + 64 * (i >> 2) + f8w::column(in >> 4, in & 15);
-            offA[i] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + chunk * 16;
-            offB[i] = (uint32_t)((col < T.cols ? col : T.cols - 1) * pitch) + chunk * 16;
+            const int in = 32 * side + 8 * (i & 3) + (lane >> 3), row = 128 * part + 64 * (i >> 2) + in;
+            offA[i] = (uint32_t)((row < T.rows ? row : T.rows - 1) * pitch) + ((lane & 7) ^ ((in & 15) >> 1)) * 16;
         }
-        // dword 4 c + f of the wave's 64: fragment f's position c
-        const int row = wave * 64 + 16 * (lane & 3) + (lane >> 2), col = wave * 64 + f8w::column(lane & 3, lane >> 2);
+#pragma unroll
+        for (int i = 0; i < FB; ++i) {
+            const int in = 16 * HB * (i / HB) + 8 * HB * side + 8 * (i % HB) + (lane >> 3), col = 16 * FB * part + f8w::column(in >> 4, in & 15);
+            offB[i] = (uint32_t)((col < T.cols ? col : T.cols - 1) * pitch) + ((lane & 7) ^ ((in & 15) >> 1)) * 16;
+        }
+        // dword 4 c + f of the wave's 64: position c of fragment 4 side + f of a part (of B those there are)
+        const int f = 4 * side + (lane & 3), row = 128 * part + 16 * f + (lane >> 2), col = 16 * FB * part + f8w::column(f < FB ? f : FB - 1, lane >> 2);
         offSA = row < T.rows ? row : T.rows - 1;
         offSB = col < T.cols ? col : T.cols - 1;
         pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT);
@@ -191,20 +201,21 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         asm volatile("s_nop 4");  // (a lane read's register as an address, five wait states later)
     };
     typedef __attribute__((address_space(3))) void *lds_ptr_t;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds, dst = __builtin_amdgcn_readfirstlane(lds0 + (first + second) * KT),
-                   dstS = __builtin_amdgcn_readfirstlane(lds0 + f8w::SCALES0 + wave * 256);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds, dstA = __builtin_amdgcn_readfirstlane(lds0 + (128 * part + 32 * side) * KT),
+                   dstB = __builtin_amdgcn_readfirstlane(lds0 + (BM + 16 * FB * part + 8 * HB * side) * KT),
+                   dstS = __builtin_amdgcn_readfirstlane(lds0 + G::SCALES0 + wave * 256);
     // load i of a K tile: of the first ones (A0, P = half ST of B, scales) and of the second (Q, A1)
     auto request_first = [&](auto st, auto i) {
         constexpr int S = decltype(st)::value, I = decltype(i)::value;
-        if constexpr (I < 4) f8w::load<S * STAGE + I * 1024>(dst, offA[I], pA);
-        else if constexpr (I < 8) f8w::load<S * STAGE + BM * KT + S * 8192 + (I - 4) * 1024>(dst, offB[4 * S + I - 4], pB);
-        else if constexpr (I == 8) f8w::load_byte<S * f8w::SCALES>(dstS, offSA, pSA);
-        else f8w::load_byte<S * f8w::SCALES + 4 * BM>(dstS, offSB, pSB);
+        if constexpr (I < 4) f8w::load<S * STAGE + I * 1024>(dstA, offA[I], pA);
+        else if constexpr (I < 4 + HB) f8w::load<S * STAGE + S * HB * 2048 + (I - 4) * 1024>(dstB, offB[HB * S + I - 4], pB);
+        else if constexpr (I == 4 + HB) f8w::load_byte<S * G::SCALES>(dstS, offSA, pSA);
+        else f8w::load_byte<S * G::SCALES + 1024>(dstS, offSB, pSB);
     };
     auto request_second = [&](auto st, auto i) {
         constexpr int S = decltype(st)::value, I = decltype(i)::value;
-        if constexpr (I < 4) f8w::load<S * STAGE + BM * KT + (1 - S) * 8192 + I * 1024>(dst, offB[4 * (1 - S) + I], pB);
-        else f8w::load<S * STAGE + 8192 + (I - 4) * 1024>(dst, offA[I], pA);
+        if constexpr (I < HB) f8w::load<S * STAGE + (1 - S) * HB * 2048 + I * 1024>(dstB, offB[HB * (1 - S) + I], pB);
+        else f8w::load<S * STAGE + 8192 + (I - HB) * 1024>(dstA, offA[4 + I - HB], pA);
     };
     auto advance = [&]() {
         pA += step;
@@ -214,7 +225,9 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     };
     auto past_end = [&]() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) offA[i] = offB[i] = 0;
+        for (int i = 0; i < 8; ++i) offA[i] = 0;
+#pragma unroll
+        for (int i = 0; i < FB; ++i) offB[i] = 0;
         offSA = offSB = 0;
         pA = P.A;
         pB = P.B;
@@ -227,16 +240,16 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     // K tiles 0 and 1 of an output tile
     auto request_start = [&](const Tile &T) {
         point_to(T);
-        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I0{}, i); });
-        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I0{}, i); });
+        f8w::each<0, G::FIRST>([&](auto i) { request_first(I0{}, i); });
+        f8w::each<0, G::SECOND>([&](auto i) { request_second(I0{}, i); });
         advance();
         if (T.count < 2) past_end();
-        f8w::each<0, f8w::FIRST>([&](auto i) { request_first(I1{}, i); });
-        f8w::each<0, f8w::SECOND>([&](auto i) { request_second(I1{}, i); });
+        f8w::each<0, G::FIRST>([&](auto i) { request_first(I1{}, i); });
+        f8w::each<0, G::SECOND>([&](auto i) { request_second(I1{}, i); });
         advance();
     };
 
-    // ---- LDS -> registers: fragment f of the wave's 128 rows of an operand
+    // ---- LDS -> registers: fragment f of the wave's rows of A, of its columns
     const int s0 = (q ^ (c >> 1)) << 4;
     const uint8_t *baseA[2][2], *baseB[2][2];  // [stage][half of the row]
 #pragma unroll
@@ -244,13 +257,13 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             baseA[s][h] = lds + s * STAGE + (wm * 128 + c) * KT + (s0 ^ (64 * h));
-            baseB[s][h] = lds + s * STAGE + (BM + wn * 128 + c) * KT + (s0 ^ (64 * h));
+            baseB[s][h] = lds + s * STAGE + (BM + wn * 16 * FB + c) * KT + (s0 ^ (64 * h));
             uint32_t v = (uint32_t)(uintptr_t)(lds_ptr_t)baseA[s][h], w = (uint32_t)(uintptr_t)(lds_ptr_t)baseB[s][h];
             asm volatile("" : "+v"(v), "+v"(w));  // (an LDS instruction's constant does not reach the second stage: bases that the compiler keeps)
             baseA[s][h] = (const uint8_t *)(lds_ptr_t)(uintptr_t)v;
             baseB[s][h] = (const uint8_t *)(lds_ptr_t)(uintptr_t)w;
         }
-    const uint8_t *baseSA = lds + f8w::SCALES0 + (wm * 128 + 4 * c) * 4, *baseSB = lds + f8w::SCALES0 + (BM + wn * 128 + 4 * c) * 4;
+    const uint8_t *baseSA = lds + G::SCALES0 + (wm * 128 + 4 * c) * 4, *baseSB = lds + G::SCALES0 + 1024 + (wn * 128 + 4 * c) * 4;
     // everything but the last n loads (and stores) has landed and all of the wave's LDS reads are done; then the same of every wave
 #define NVFP4_F8W_WAIT(n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(n) : "memory");
 #define NVFP4_F8W_BARRIER               \
@@ -266,18 +279,18 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     NVFP4_F8W_WAIT(ALL)
     while (true) {
         // here: K tile 0 has landed, as far as this wave is concerned
-        float4v_t acc[8][8];
+        float4v_t acc[8][FB];
 #pragma unroll
         for (int a = 0; a < 8; ++a)
 #pragma unroll
-            for (int b = 0; b < 8; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-        Codes A[8], B[8];
+            for (int b = 0; b < FB; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
+        Codes A[8], B[FB];
         auto read_a = [&](int st, int f, int h) { (h ? A[f].hi : A[f].lo) = *reinterpret_cast<const u32x4_t *>(baseA[st][h] + 16 * f * KT); };
         auto read_b = [&](int st, int f, int h) { (h ? B[f].hi : B[f].lo) = *reinterpret_cast<const u32x4_t *>(baseB[st][h] + 16 * f * KT); };
         // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
         u32x4_t SA[2][2], SB[2][2];
         auto read_scales = [&](int st, int i) {
-            (i < 2 ? SA[st][i & 1] : SB[st][i & 1]) = *reinterpret_cast<const u32x4_t *>((i < 2 ? baseSA : baseSB) + st * f8w::SCALES + (i & 1) * 256);
+            (i < 2 ? SA[st][i & 1] : SB[st][i & 1]) = *reinterpret_cast<const u32x4_t *>((i < 2 ? baseSA : baseSB) + st * G::SCALES + (i & 1) * 256);
         };
             int kt = 0;
         // stage ST, which is also the half P of B
@@ -290,37 +303,40 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             __builtin_amdgcn_sched_barrier(0);
             // MFMA j of a quarter: along a row of tiles and back along the next, one operand changes at a time
             auto quarter = [&](auto ha, auto hb, auto &&between) {
-                f8w::each<0, 16>([&](auto j) {
-                    constexpr int J = decltype(j)::value, r = J >> 2, i = r & 1 ? 3 - (J & 3) : J & 3;
-                    constexpr int a = 4 * decltype(ha)::value + r, b = 4 * decltype(hb)::value + i;
+                f8w::each<0, 4 * HB>([&](auto j) {
+                    constexpr int J = decltype(j)::value, r = J / HB, i = r & 1 ? HB - 1 - J % HB : J % HB;
+                    constexpr int a = 4 * decltype(ha)::value + r, b = HB * decltype(hb)::value + i;
                     f8w::mfma(acc[a][b], B[b].all(), A[a].all(), SB[ST][b >> 2][b & 3], SA[ST][a >> 2][a & 3]);
                     __builtin_amdgcn_sched_barrier(0);
                     between(j);
                     __builtin_amdgcn_sched_barrier(0);
                 });
             };
+            // what goes between the MFMAs, N things from MFMA `from` on, spread over those that are left
+            auto spread = [&](auto j, auto from, auto n, auto &&f) {
+                constexpr int J = decltype(j)::value, F = decltype(from)::value, N = decltype(n)::value, L = 4 * HB - F;
+                if constexpr (J >= F) f8w::each<(J - F) * N / L, (J - F + 1) * N / L>(f);
+            };
+            using F0 = std::integral_constant<int, 0>;
+            using FH = std::integral_constant<int, 2 * HB>;
+            using Frags = std::integral_constant<int, 8>;
             quarter(I0{}, HP{}, [&](auto j) {
-                constexpr int J = decltype(j)::value;
-                if constexpr (J < 8) read_b(ST, 4 * (1 - ST) + (J >> 1), J & 1);
-                if constexpr (J >= 16 - f8w::FIRST) request_first(stage, std::integral_constant<int, J - (16 - f8w::FIRST)>{});
+                if constexpr (decltype(j)::value < 2 * HB) read_b(ST, HB * (1 - ST) + (decltype(j)::value >> 1), decltype(j)::value & 1);
+                spread(j, std::integral_constant<int, 4 * HB - (G::FIRST < 3 * HB ? G::FIRST : 3 * HB)>{}, std::integral_constant<int, G::FIRST>{},
+                       [&](auto i) { request_first(stage, i); });
             });
-            quarter(I0{}, HQ{}, [&](auto j) {
-                constexpr int J = decltype(j)::value;
-                if constexpr (J < 8) read_a(ST, 4 + (J >> 1), J & 1);
-            });
+            quarter(I0{}, HQ{}, [&](auto j) { spread(j, F0{}, Frags{}, [&](auto i) { read_a(ST, 4 + (decltype(i)::value >> 1), decltype(i)::value & 1); }); });
             NVFP4_F8W_WAIT(ALL)
             NVFP4_F8W_BARRIER
             __builtin_amdgcn_sched_barrier(0);
             quarter(I1{}, HQ{}, [&](auto j) {
-                constexpr int J = decltype(j)::value;
-                if constexpr (J < 8) read_a(1 - ST, J >> 1, J & 1);
-                if constexpr (J >= 8) request_second(stage, std::integral_constant<int, J - 8>{});
+                spread(j, F0{}, Frags{}, [&](auto i) { read_a(1 - ST, decltype(i)::value >> 1, decltype(i)::value & 1); });
+                spread(j, FH{}, std::integral_constant<int, G::SECOND>{}, [&](auto i) { request_second(stage, i); });
             });
             advance();
             quarter(I1{}, HP{}, [&](auto j) {
-                constexpr int J = decltype(j)::value;
-                if constexpr (J < 8) read_b(1 - ST, 4 * (1 - ST) + (J >> 1), J & 1);
-                if constexpr (J >= 8 && J < 12) read_scales(1 - ST, J - 8);
+                if constexpr (decltype(j)::value < 2 * HB) read_b(1 - ST, HB * (1 - ST) + (decltype(j)::value >> 1), decltype(j)::value & 1);
+                spread(j, FH{}, std::integral_constant<int, 4>{}, [&](auto i) { read_scales(1 - ST, decltype(i)::value); });
             });
             NVFP4_F8W_WAIT(ALL)
             NVFP4_F8W_BARRIER
@@ -332,7 +348,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 read_a(0, f, h);
-                read_b(0, f, h);
+                if (f < HB) read_b(0, f, h);
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) read_scales(0, i);
@@ -352,29 +368,30 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             request_start(next);
         }
         asm volatile("s_nop 15" ::: "memory");
-        // The next tile's first K tile has landed when its second and what was stored behind that (32 stores inside the output, as few as none at its
+        // The next tile's first K tile has landed when its second and what was stored behind that (STORES inside the output, as few as none at its
         // edge) are all that is outstanding.
-        auto store = [&](auto inside) {
+        auto store = [&](auto inside, auto streamed) {
             int at_lane = lane;
             asm volatile("" : "+v"(at_lane));  // (or the addresses are computed before the K loop and kept)
             const int c = at_lane & 15, q = at_lane >> 4;
 #pragma unroll
             for (int a = 0; a < 8; ++a)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const int row = wm * 128 + 16 * a + c, col = wn * 128 + 32 * s + 8 * q;
+                for (int s = 0; s < HB; ++s) {
+                    const int row = wm * 128 + 16 * a + c, col = wn * 16 * FB + 32 * s + 8 * q;
                     float v[8];
                     // (reads that stay behind the wait states and leave the accumulators alone)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
                     const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + col;
-                    if constexpr (decltype(inside)::value != 0) store_eight(P.out, at, v, 8, keep);
-                    else if (row < T.rows && col < T.cols) store_eight(P.out, at, v, T.cols - col, keep);
+                    if constexpr (decltype(inside)::value != 0) store_eight<(decltype(streamed)::value != 0)>(P.out, at, v, 8, keep);
+                    else if (row < T.rows && col < T.cols) store_eight<false>(P.out, at, v, T.cols - col, keep);
                 }
-            NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? 32 : 0))
+            NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
         };
-        if (T.rows == BM && T.cols == BN) store(I1{});
-        else store(I0{});
+        if (T.rows != BM || T.cols != BN) store(I0{}, I0{});
+        else if (P.stream) store(I1{}, I1{});
+        else store(I1{}, I0{});
         if (id >= tiles) break;
         T = next;
         keep = next_keep;
@@ -385,7 +402,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 }
 
 // Of the current device; a multiple of 8, so that a workgroup's tiles stay on its XCD's part of the walk
-static int64_t compute_units()
+int64_t compute_units()
 {
     static std::atomic<int> known[64];
     int device = 0, n = 0;
@@ -397,29 +414,59 @@ static int64_t compute_units()
     return n;
 }
 
-template <int MODE>
+template <int MODE, int FB>
 static hipError_t launch_wide(const Fp8GemmArgs &P, hipStream_t st)
 {
-    auto *k = fp8_gemm_wide_kernel<MODE>;
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, f8w::LDS_BYTES);
+    using G = f8w::Geom<FB>;
+    auto *k = fp8_gemm_wide_kernel<MODE, FB>;
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS_BYTES);
     if (once != hipSuccess) return once;
-    const int64_t tiles = f8g::tiles<MODE>(P, f8w::BM, f8w::BN), cus = compute_units();
-    k<<<dim3((unsigned)(tiles < cus ? tiles : cus)), 256, f8w::LDS_BYTES, st>>>(P);
+    const int64_t tiles = f8g::tiles<MODE>(P, f8w::BM, G::BN), cus = compute_units();
+    k<<<dim3((unsigned)(tiles < cus ? tiles : cus)), 256, G::LDS_BYTES, st>>>(P);
     return hipGetLastError();
 }
 
-bool fp8_gemm_is_wide(const Fp8GemmArgs &P, int mode)
+// Time of a K tile on every CU, us, by the tile's width (4096 x 4096 x 4096 and 2048 x 4096 x 4096, where tiles are one round and fewer than the CUs)
+constexpr double K_TILE_128 = 0.67, K_TILE_192 = 0.92, K_TILE_256 = 1.2;
+
+// The tile's width: fewest rounds of the CUs, weighted by what a round takes.  us, 128 / 192 / 256 columns: 777 x 12288 x 4096 57 / 45 / 54, 4096 x 4096 x 4096
+// 64 / 76 / 54, 2048 x 4096 x 4096 30 / 36 / 44, 2048 x 11008 x 4096 100 / 86 / 100, 4096 x 11008 x 4096 186 / 158 / 146, 3000 x 3000 x 1024 21 / 16 / 18,
+// experts 4096 x 2 of 8, 4096 x 4096 134 / 144 / 139, 8192 x 2 of 16, 4096 x 2048 168 / 166 / 146.
+static int width_of(const Fp8GemmArgs &P, int mode, double *cost)
 {
-    if (P.blocks == 0) return false;
-    const int64_t ntx = (P.N + 255) / 256;
-    if (mode == FP8_DENSE) return ntx * ((P.M + 255) / 256) >= 128;
-    if (mode == FP8_EXPERTS) return ntx * (P.M / 256) >= 128 && P.M >= 128 * (int64_t)P.groups;
-    return ntx * ((P.M + 255) / 256) * P.groups >= 128;
+    // (an expert's last tile of rows is half full on average)
+    const int64_t cus = compute_units(), rows = mode == FP8_EXPERTS ? P.M / 256 + (P.groups + 1) / 2 : (P.M + 255) / 256 * (mode == FP8_EXPERTS_DW ? P.groups : 1);
+    const double k_tile[3] = {K_TILE_128, K_TILE_192, K_TILE_256};
+    int best = 4;
+    *cost = 1e30;
+    for (int fb = 4; fb <= 8; fb += 2) {
+        const double c = (double)((rows * ((P.N + 32 * fb - 1) / (32 * fb)) + cus - 1) / cus) * k_tile[fb / 2 - 2];
+        if (c < *cost) {
+            *cost = c;
+            best = fb;
+        }
+    }
+    return best;
+}
+
+double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode)
+{
+    double cost;
+    width_of(P, mode, &cost);
+    return cost;
+}
+
+template <int MODE>
+static hipError_t launch_width(const Fp8GemmArgs &P, hipStream_t st)
+{
+    double cost;
+    const int fb = width_of(P, MODE, &cost);
+    return fb == 4 ? launch_wide<MODE, 4>(P, st) : fb == 6 ? launch_wide<MODE, 6>(P, st) : launch_wide<MODE, 8>(P, st);
 }
 
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, hipStream_t st)
 {
-    return mode == FP8_DENSE ? launch_wide<FP8_DENSE>(P, st) : mode == FP8_EXPERTS ? launch_wide<FP8_EXPERTS>(P, st) : launch_wide<FP8_EXPERTS_DW>(P, st);
+    return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, st) : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, st) : launch_width<FP8_EXPERTS_DW>(P, st);
 }
 
 }  // namespace nvfp4
