@@ -73,11 +73,11 @@ struct Fp8GemmArgs {
     int32_t stream;                       // the output leaves by nontemporal stores (set by launch_fp8_gemm())
 };
 // The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
-// few tiles; 256 rows by 128 to 256 columns, bf16 outputs; 128 x 128.
+// few tiles; 256 rows by 128 to 256 columns (binary32 outputs: 128); 128 x 128.
 double fp8_gemm_thin_cost(const Fp8GemmArgs &P, int mode);
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
-double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode);
-hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, hipStream_t st);
+double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt);
+hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 int64_t compute_units();
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 

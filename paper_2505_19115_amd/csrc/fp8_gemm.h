@@ -132,10 +132,10 @@ __device__ __forceinline__ Expanded expand(const Codes &x, uint32_t byte)
         }
     return r;
 }
-__device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, const Expanded &a)
+// step i of four
+__device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, const Expanded &a, int i)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], acc, 0, 0, 0);
 }
 
 // n of four columns of one row
@@ -165,6 +165,22 @@ __device__ __forceinline__ void store_four(void *out, int64_t at, const float4v_
             for (int i = 0; i < 3; ++i)
                 if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
         }
+    }
+}
+
+// n of four columns of one row, in binary32
+template <bool STREAMED>
+__device__ __forceinline__ void store_words(void *out, int64_t at, const u32x4_t &w, int n)
+{
+    typedef u32x4_t __attribute__((aligned(4))) anywhere_t;
+    uint32_t *const p = reinterpret_cast<uint32_t *>(out) + at;
+    if (n >= 4) {
+        if (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<anywhere_t *>(p));
+        else *reinterpret_cast<anywhere_t *>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = w[i];
     }
 }
 

@@ -84,7 +84,9 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
             for (int b = 0; b < 4; ++b) {
                 const Expanded fb = expand(read(B, b), (sb >> (8 * b)) & 255);
 #pragma unroll
-                for (int a = 0; a < 4; ++a) multiply(acc[a][b], fb, fa[a]);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int a = 0; a < 4; ++a) multiply(acc[a][b], fb, fa[a], i);
             }
         } else {
             int8v_t fa[4], fb[4];
@@ -124,7 +126,7 @@ static hipError_t launch_tiles(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 }
 
 // Per K tile: us of a round of these tiles, two workgroups a CU
-constexpr double K_TILE_BF16 = 0.85, K_TILE_F32 = 2.0;
+constexpr double K_TILE_BF16 = 0.85, K_TILE_F32 = 2.2;
 
 template <int MODE>
 static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
@@ -134,18 +136,19 @@ static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
     P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * 2 > ((int64_t)256 << 20);
     const int64_t mine = f8g::tiles<MODE>(P, 128, 128), slots = 2 * compute_units();
     const double cost = (double)((mine + slots - 1) / slots) * (out_dt == NVFP4_F32 ? K_TILE_F32 : K_TILE_BF16);
-    const double wide = out_dt == NVFP4_BF16 && P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE) : 1e30;
+    const double wide = P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE, out_dt) : 1e30;
     // An expert's few rows: 8 on average for bf16, 16 for binary32 (us, few rows / tiles: 64 tokens, 8 of 64, 1024 x 2048 38 / 40 and 39 / 68; 128 tokens 51 / 41 and
     // 51 / 68; 64 tokens, 2 of 8, 4096 x 4096 51 / 30 and 52 / 74)
     if (MODE == FP8_EXPERTS && P.M <= (out_dt == NVFP4_BF16 ? 8 : 16) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     if (MODE == FP8_DENSE) {
-        const double thin = fp8_gemm_thin_cost(P, MODE);
+        // (expanding codes for binary32: 2000 x 2000 x 2000 44 / 34, 1056 x 2080 x 2784 36 / 43)
+        const double thin = fp8_gemm_thin_cost(P, MODE) * (out_dt == NVFP4_F32 ? 1.3 : 1.0);
         if (thin < cost && thin < wide) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     }
     // A short contraction in few tiles: the larger ones take 1 to 2 us more to begin and end (experts 300 tokens, 3 of 10, 500 x 700 8.7 / 10.5, their weight
     // gradients 7.1 / 8.5)
     const int32_t count = MODE == FP8_EXPERTS_DW ? P.blocks / P.groups : P.blocks;
-    if (wide < cost && !(count <= 6 && mine <= slots / 2)) return launch_fp8_gemm_wide(P, (Fp8Mode)MODE, st);
+    if (wide < cost && !(count <= 6 && mine <= slots / 2)) return launch_fp8_gemm_wide(P, (Fp8Mode)MODE, out_dt, st);
     return launch_tiles<MODE>(P, out_dt, st);
 }
 

@@ -62,11 +62,16 @@ __global__ __launch_bounds__(64 * NW) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
         for (int u = 0; u < U; ++u) {
             if (kt + u * NW < T.count) {
                 if constexpr (OUT_DT == NVFP4_F32) {
+                    Expanded ea[MT];
+#pragma unroll
+                    for (int a = 0; a < MT; ++a) ea[a] = expand(fa[u][a], sa[u][a]);
 #pragma unroll
                     for (int b = 0; b < TN; ++b) {
                         const Expanded eb = expand(fb[u][b], sb[u][b]);
 #pragma unroll
-                        for (int a = 0; a < MT; ++a) multiply(acc[a][b], eb, expand(fa[u][a], sa[u][a]));
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int a = 0; a < MT; ++a) multiply(acc[a][b], eb, ea[a], i);
                     }
                 } else {
 #pragma unroll

@@ -1,4 +1,4 @@
-// 8-bit products with bf16 outputs on 256 x 256 tiles: 2 x 2 waves of 128 x 128 (8 x 8 MFMA tiles of 16 x 16, all 256 accumulator registers, one
+// 8-bit products on tiles of 256 rows by up to 256 columns: 2 x 2 waves of 128 x 128 (8 x 8 MFMA tiles of 16 x 16, all 256 accumulator registers, one
 // wave per SIMD).  A K tile is 64 MFMAs a wave, 32 cycles each, and 128 KB out of the LDS for the four of them, half of what it delivers
 // in that time.
 //
@@ -30,17 +30,21 @@ namespace f8w {
 
 constexpr int BM = 256, KT = FP8_BLOCK;
 // FB: fragments of 16 columns of a wave; the workgroup's tile is 256 x 32 FB
-template <int FB>
+template <int FB, int OUT_DT>
 struct Geom {
     static constexpr int BN = 32 * FB, HB = FB / 2;                     // fragments of a half of B
     static constexpr int STAGE = (BM + BN) * KT, SCALES = 4 * 512;     // of a K tile; scale bytes: a dword for each of 8 fragments a wave
     static constexpr int SCALES0 = 2 * STAGE, GROUPS0 = SCALES0 + 2 * SCALES, LDS_BYTES = GROUPS0 + 2 * 4 * (MAX_EXPERTS + 2);
     static constexpr int FIRST = 4 + HB + 2, SECOND = HB + 4;           // loads of a wave and K tile: A0, P and scales; Q and A1
-    static constexpr int STORES = 4 * FB;                               // of a wave, for an output inside
+    static constexpr int STORES = (OUT_DT == NVFP4_F32 ? 8 : 4) * FB;  // of a wave, for an output inside
 };
 
-// Column (of the wave's) that position c of fragment f holds
-__device__ __forceinline__ int column(int f, int c) { return 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3); }
+// Column (of the wave's) that position c of fragment f holds: a lane ends with columns of one row that fill 16 bytes
+template <int OUT_DT>
+__device__ __forceinline__ int column(int f, int c)
+{
+    return OUT_DT == NVFP4_F32 ? 16 * f + c : 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3);
+}
 
 // As assembly, so that the 64 accumulators stay where they are (gemm_mx.hip).  What the compiler does not know about it: an operand must not have been
 // written by the vector ALU in the two instructions before (they come from LDS reads), and the last result must not be read for 11 wait
@@ -75,11 +79,11 @@ __device__ __forceinline__ void each(F &&f)
 
 }  // namespace f8w
 
-template <int MODE, int FB>
+template <int MODE, int OUT_DT, int FB>
 __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 {
     using namespace f8g;
-    using G = f8w::Geom<FB>;
+    using G = f8w::Geom<FB, OUT_DT>;
     constexpr int BM = f8w::BM, BN = G::BN, HB = G::HB, STAGE = G::STAGE, ALL = G::FIRST + G::SECOND;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
@@ -184,11 +188,11 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         }
 #pragma unroll
         for (int i = 0; i < FB; ++i) {
-            const int in = 16 * HB * (i / HB) + 8 * HB * side + 8 * (i % HB) + (lane >> 3), col = 16 * FB * part + f8w::column(in >> 4, in & 15);
+            const int in = 16 * HB * (i / HB) + 8 * HB * side + 8 * (i % HB) + (lane >> 3), col = 16 * FB * part + f8w::column<OUT_DT>(in >> 4, in & 15);
             offB[i] = (uint32_t)((col < T.cols ? col : T.cols - 1) * pitch) + ((lane & 7) ^ ((in & 15) >> 1)) * 16;
         }
         // dword 4 c + f of the wave's 64: position c of fragment 4 side + f of a part (of B those there are)
-        const int f = 4 * side + (lane & 3), row = 128 * part + 16 * f + (lane >> 2), col = 16 * FB * part + f8w::column(f < FB ? f : FB - 1, lane >> 2);
+        const int f = 4 * side + (lane & 3), row = 128 * part + 16 * f + (lane >> 2), col = 16 * FB * part + f8w::column<OUT_DT>(f < FB ? f : FB - 1, lane >> 2);
         offSA = row < T.rows ? row : T.rows - 1;
         offSB = col < T.cols ? col : T.cols - 1;
         pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT);
@@ -301,6 +305,53 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             if (kt + 2 >= T.count) past_end();
             asm volatile("s_nop 1");  // (accumulators that were just cleared: two instructions between that and the MFMAs)
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (OUT_DT == NVFP4_F32) {
+                // Halves as bf16: of A the one that is multiplied, of B both.  The compiler arranges what is between the barriers.
+                Expanded EA[4], EB[FB];
+                auto expand_a = [&](int h) {
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) EA[f] = expand(A[4 * h + f], SA[ST][h][f]);
+                };
+                auto expand_b = [&](int h) {
+#pragma unroll
+                    for (int f = HB * h; f < HB * h + HB; ++f) EB[f] = expand(B[f], SB[ST][f >> 2][f & 3]);
+                };
+                auto quarter = [&](int ha, int hb) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int f = HB * hb; f < HB * hb + HB; ++f)
+#pragma unroll
+                            for (int a = 0; a < 4; ++a) multiply(acc[4 * ha + a][f], EB[f], EA[a], i);
+                };
+                f8w::each<0, G::FIRST>([&](auto i) { request_first(stage, i); });
+                expand_a(0);
+                expand_b(ST);
+#pragma unroll
+                for (int i = 0; i < 2 * HB; ++i) read_b(ST, HB * (1 - ST) + (i >> 1), i & 1);
+                quarter(0, ST);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read_a(ST, 4 + (i >> 1), i & 1);
+                expand_b(1 - ST);
+                quarter(0, 1 - ST);
+                NVFP4_F8W_WAIT(ALL)
+                NVFP4_F8W_BARRIER
+                f8w::each<0, G::SECOND>([&](auto i) { request_second(stage, i); });
+                expand_a(1);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) read_a(1 - ST, i >> 1, i & 1);
+                quarter(1, 1 - ST);
+#pragma unroll
+                for (int i = 0; i < 2 * HB; ++i) read_b(1 - ST, HB * (1 - ST) + (i >> 1), i & 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) read_scales(1 - ST, i);
+                quarter(1, ST);
+                advance();
+                NVFP4_F8W_WAIT(ALL)
+                NVFP4_F8W_BARRIER
+                ++kt;
+                return;
+            }
             // MFMA j of a quarter: along a row of tiles and back along the next, one operand changes at a time
             auto quarter = [&](auto ha, auto hb, auto &&between) {
                 f8w::each<0, 4 * HB>([&](auto j) {
@@ -375,7 +426,18 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             asm volatile("" : "+v"(at_lane));  // (or the addresses are computed before the K loop and kept)
             const int c = at_lane & 15, q = at_lane >> 4;
 #pragma unroll
-            for (int a = 0; a < 8; ++a)
+            for (int a = 0; a < 8; ++a) {
+                if constexpr (OUT_DT == NVFP4_F32) {
+#pragma unroll
+                    for (int b = 0; b < FB; ++b) {
+                        const int row = wm * 128 + 16 * a + c, col = wn * 16 * FB + 16 * b + 4 * q;
+                        const u32x4_t w = __builtin_bit_cast(u32x4_t, acc[a][b]) & keep;
+                        const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + col;
+                        if constexpr (decltype(inside)::value != 0) store_words<(decltype(streamed)::value != 0)>(P.out, at, w, 4);
+                        else if (row < T.rows && col < T.cols) store_words<false>(P.out, at, w, T.cols - col);
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int s = 0; s < HB; ++s) {
                     const int row = wm * 128 + 16 * a + c, col = wn * 16 * FB + 32 * s + 8 * q;
@@ -387,6 +449,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                     if constexpr (decltype(inside)::value != 0) store_eight<(decltype(streamed)::value != 0)>(P.out, at, v, 8, keep);
                     else if (row < T.rows && col < T.cols) store_eight<false>(P.out, at, v, T.cols - col, keep);
                 }
+            }
             NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
         };
         if (T.rows != BM || T.cols != BN) store(I0{}, I0{});
@@ -414,11 +477,11 @@ int64_t compute_units()
     return n;
 }
 
-template <int MODE, int FB>
+template <int MODE, int OUT_DT, int FB>
 static hipError_t launch_wide(const Fp8GemmArgs &P, hipStream_t st)
 {
-    using G = f8w::Geom<FB>;
-    auto *k = fp8_gemm_wide_kernel<MODE, FB>;
+    using G = f8w::Geom<FB, OUT_DT>;
+    auto *k = fp8_gemm_wide_kernel<MODE, OUT_DT, FB>;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS_BYTES);
     if (once != hipSuccess) return once;
     const int64_t tiles = f8g::tiles<MODE>(P, f8w::BM, G::BN), cus = compute_units();
@@ -427,20 +490,20 @@ static hipError_t launch_wide(const Fp8GemmArgs &P, hipStream_t st)
 }
 
 // Time of a K tile on every CU, us, by the tile's width (4096 x 4096 x 4096 and 2048 x 4096 x 4096, where tiles are one round and fewer than the CUs)
-constexpr double K_TILE_128 = 0.67, K_TILE_192 = 0.92, K_TILE_256 = 1.2;
+constexpr double K_TILE_128 = 0.67, K_TILE_192 = 0.92, K_TILE_256 = 1.2, K_TILE_F32 = 1.85;
 
 // The tile's width: fewest rounds of the CUs, weighted by what a round takes.  us, 128 / 192 / 256 columns: 777 x 12288 x 4096 57 / 45 / 54, 4096 x 4096 x 4096
 // 64 / 76 / 54, 2048 x 4096 x 4096 30 / 36 / 44, 2048 x 11008 x 4096 100 / 86 / 100, 4096 x 11008 x 4096 186 / 158 / 146, 3000 x 3000 x 1024 21 / 16 / 18,
 // experts 4096 x 2 of 8, 4096 x 4096 134 / 144 / 139, 8192 x 2 of 16, 4096 x 2048 168 / 166 / 146.
-static int width_of(const Fp8GemmArgs &P, int mode, double *cost)
+static int width_of(const Fp8GemmArgs &P, int mode, int out_dt, double *cost)
 {
     // (an expert's last tile of rows is half full on average)
     const int64_t cus = compute_units(), rows = mode == FP8_EXPERTS ? P.M / 256 + (P.groups + 1) / 2 : (P.M + 255) / 256 * (mode == FP8_EXPERTS_DW ? P.groups : 1);
     const double k_tile[3] = {K_TILE_128, K_TILE_192, K_TILE_256};
     int best = 4;
     *cost = 1e30;
-    for (int fb = 4; fb <= 8; fb += 2) {
-        const double c = (double)((rows * ((P.N + 32 * fb - 1) / (32 * fb)) + cus - 1) / cus) * k_tile[fb / 2 - 2];
+    for (int fb = 4; fb <= (out_dt == NVFP4_F32 ? 4 : 8); fb += 2) {
+        const double c = (double)((rows * ((P.N + 32 * fb - 1) / (32 * fb)) + cus - 1) / cus) * (out_dt == NVFP4_F32 ? K_TILE_F32 : k_tile[fb / 2 - 2]);
         if (c < *cost) {
             *cost = c;
             best = fb;
@@ -449,24 +512,25 @@ static int width_of(const Fp8GemmArgs &P, int mode, double *cost)
     return best;
 }
 
-double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode)
+double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt)
 {
     double cost;
-    width_of(P, mode, &cost);
+    width_of(P, mode, out_dt, &cost);
     return cost;
 }
 
 template <int MODE>
-static hipError_t launch_width(const Fp8GemmArgs &P, hipStream_t st)
+static hipError_t launch_width(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
+    if (out_dt == NVFP4_F32) return launch_wide<MODE, NVFP4_F32, 4>(P, st);
     double cost;
-    const int fb = width_of(P, MODE, &cost);
-    return fb == 4 ? launch_wide<MODE, 4>(P, st) : fb == 6 ? launch_wide<MODE, 6>(P, st) : launch_wide<MODE, 8>(P, st);
+    const int fb = width_of(P, MODE, out_dt, &cost);
+    return fb == 4 ? launch_wide<MODE, NVFP4_BF16, 4>(P, st) : fb == 6 ? launch_wide<MODE, NVFP4_BF16, 6>(P, st) : launch_wide<MODE, NVFP4_BF16, 8>(P, st);
 }
 
-hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, hipStream_t st)
+hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
 {
-    return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, st) : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, st) : launch_width<FP8_EXPERTS_DW>(P, st);
+    return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, out_dt, st) : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, out_dt, st) : launch_width<FP8_EXPERTS_DW>(P, out_dt, st);
 }
 
 }  // namespace nvfp4

@@ -6,6 +6,8 @@
 //   combine       out[t] = sum_j w[t, j] y[position[t, j]], choices in their order, binary32
 //   combine_bwd   dy[position[t, j]] = w[t, j] dout[t],  dw[t, j] = sum_d dout[t, d] y[position[t, j], d]
 // All of it is bound by memory; a wave moves a row (of a pair, or of a token with its choices) in pieces of 16 bytes a lane.
+#include <type_traits>
+
 #include "experts.h"
 
 namespace nvfp4 {
@@ -196,9 +198,11 @@ struct Piece {
     struct __attribute__((packed, aligned(2))) P2 { u32x4_t w; };
     struct __attribute__((packed, aligned(4))) P4 { u32x4_t w; };
     u32x4_t w;
+    template <bool STREAMED>
     __device__ __forceinline__ void load(const uint8_t *p)
     {
-        w = DT == NVFP4_BF16 ? reinterpret_cast<const P2 *>(p)->w : reinterpret_cast<const P4 *>(p)->w;
+        if (STREAMED) w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+        else w = DT == NVFP4_BF16 ? reinterpret_cast<const P2 *>(p)->w : reinterpret_cast<const P4 *>(p)->w;
     }
     __device__ __forceinline__ void store(uint8_t *p) const
     {
@@ -243,21 +247,52 @@ struct Piece {
     }
 };
 
-// Calls body(offset in bytes, elements there) for a lane's pieces of a row: whole pieces first, U of them side by side
-template <int DT, class F>
-__device__ __forceinline__ void pieces(int64_t cols, int lane, F &&body)
+// Walks a row in steps of U pieces a lane: body(at, n) with the byte offsets of a lane's pieces and how many elements each has there (0: none), and
+// whether all of them are whole, which is the same in the wave.
+template <int DT, int U, class F>
+__device__ __forceinline__ void walk(int64_t cols, int lane, F &&body)
 {
     constexpr int N = Piece<DT>::N;
-    for (int64_t i = (int64_t)lane * N; i < cols; i += 64 * N) body(i * Piece<DT>::ESZ, (int)(cols - i < N ? cols - i : N));
+    for (int64_t c0 = 0; c0 < cols; c0 += 64 * N * U) {
+        int64_t at[U];
+        int n[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = c0 + (u * 64 + lane) * N;
+            at[u] = c * Piece<DT>::ESZ;
+            n[u] = c + N <= cols ? N : c < cols ? (int)(cols - c) : 0;
+        }
+        if (c0 + 64 * N * U <= cols) body(at, n, std::true_type{});
+        else body(at, n, std::false_type{});
+    }
+}
+template <int DT, bool WHOLE, bool STREAMED, int U>
+__device__ __forceinline__ void load(Piece<DT> (&v)[U], const uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (WHOLE || n[u] == Piece<DT>::N) v[u].template load<STREAMED>(row + at[u]);
+        else v[u].load_some(row + at[u], n[u]);
+    }
+}
+template <int DT, bool WHOLE, int U>
+__device__ __forceinline__ void store(const Piece<DT> (&v)[U], uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (WHOLE || n[u] == Piece<DT>::N) v[u].store(row + at[u]);
+        else v[u].store_some(row + at[u], n[u]);
+    }
 }
 
 }  // namespace moe
 
-template <int DT>
+template <int DT, bool STREAMED>
 __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k,
                                                          int64_t rows, uint8_t *out)
 {
     using namespace moe;
+    constexpr int U = 2;
     const int lane = threadIdx.x & 63;
     const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (r >= rows) return;
@@ -265,67 +300,77 @@ __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64
     const int64_t src = pair < 0 || pair / top_k >= x_rows ? -1 : pair / top_k;
     const uint8_t *const from = x + src * ld * Piece<DT>::ESZ;
     uint8_t *const to = out + r * cols * Piece<DT>::ESZ;
-    pieces<DT>(cols, lane, [&](int64_t at, int n) {
-        Piece<DT> v;
-        v.w = u32x4_t{0, 0, 0, 0};
-        if (n == Piece<DT>::N) {
-            if (src >= 0) v.load(from + at);
-            v.store(to + at);
+    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        Piece<DT> v[U];
+        if (src >= 0) {
+            load<DT, W, STREAMED>(v, from, at, n);
         } else {
-            if (src >= 0) v.load_some(from + at, n);
-            v.store_some(to + at, n);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
         }
+        store<DT, W>(v, to, at, n);
     });
 }
 
-template <int DT>
+// A wave for each token.  Two choices at a time: as many loads in flight.
+template <int DT, bool STREAMED>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position,
                                                           int64_t tokens, int32_t top_k, uint8_t *out)
 {
     using namespace moe;
+    constexpr int U = 2, N = Piece<DT>::N;
     const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = cols * Piece<DT>::ESZ;
     if (t >= tokens) return;
-    pieces<DT>(cols, lane, [&](int64_t at, int n) {
-        float sum[Piece<DT>::N];
+    const int32_t *const places = position + t * top_k;
+    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        float sum[U][N];
 #pragma unroll
-        for (int i = 0; i < Piece<DT>::N; ++i) sum[i] = 0.0f;
-        for (int j = 0; j < top_k; ++j) {
-            const int32_t p = position[t * top_k + j];
-            if (p < 0 || p >= y_rows) continue;
-            const float w = weights ? weights[t * top_k + j] : 1.0f;
-            Piece<DT> v;
-            const uint8_t *const from = y + ((int64_t)p * cols) * Piece<DT>::ESZ + at;
-            if (n == Piece<DT>::N) v.load(from);
-            else v.load_some(from, n);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < Piece<DT>::N; ++i) sum[i] = __builtin_fmaf(w, v.get(i), sum[i]);
+            for (int i = 0; i < N; ++i) sum[u][i] = 0.0f;
+        auto add = [&](const Piece<DT> (&v)[U], float w) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[u][i] = __builtin_fmaf(w, v[u].get(i), sum[u][i]);
+        };
+        for (int j = 0; j < top_k; j += 2) {
+            const int32_t p = places[j], q = j + 1 < top_k ? places[j + 1] : -1;
+            const bool has_p = p >= 0 && p < y_rows, has_q = q >= 0 && q < y_rows;
+            Piece<DT> a[U], b[U];
+            if (has_p) load<DT, W, STREAMED>(a, y + p * row, at, n);
+            if (has_q) load<DT, W, STREAMED>(b, y + q * row, at, n);
+            if (has_p) add(a, weights ? weights[t * top_k + j] : 1.0f);
+            if (has_q) add(b, weights ? weights[t * top_k + j + 1] : 1.0f);
         }
-        Piece<DT> v;
-        v.set(sum);
-        if (n == Piece<DT>::N) v.store(out + t * cols * Piece<DT>::ESZ + at);
-        else v.store_some(out + t * cols * Piece<DT>::ESZ + at, n);
+        Piece<DT> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].set(sum[u]);
+        store<DT, W>(v, out + t * row, at, n);
     });
 }
 
 // A wave for each pair; behind them the waves that clear the rows of dy past the last kept pair
-template <int DT>
+template <int DT, bool STREAMED>
 __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dout, const uint8_t *y, int64_t rows, int64_t cols, const float *weights,
                                                               const int32_t *position, const int32_t *kept, int64_t pairs, int32_t top_k, uint8_t *dy,
                                                               float *dweights)
 {
     using namespace moe;
-    constexpr int N = Piece<DT>::N;
+    constexpr int U = 2, N = Piece<DT>::N;
     const int lane = threadIdx.x & 63;
     const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = cols * Piece<DT>::ESZ;
     if (id >= pairs) {
         const int64_t clearing = (int64_t)gridDim.x * 4 - pairs;
         for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
-            pieces<DT>(cols, lane, [&](int64_t at, int n) {
-                Piece<DT> v;
-                v.w = u32x4_t{0, 0, 0, 0};
-                if (n == N) v.store(dy + r * row + at);
-                else v.store_some(dy + r * row + at, n);
+            walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+                Piece<DT> v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
+                store<DT, decltype(whole)::value>(v, dy + r * row, at, n);
             });
         return;
     }
@@ -338,34 +383,44 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
     uint8_t *const to = dy + p * row;
     const float w = weights[id];
     float dot = 0.0f;
-    pieces<DT>(cols, lane, [&](int64_t at, int n) {
-        Piece<DT> a, b;
-        if (n == N) {
-            a.load(up + at);
-            b.load(from + at);
-        } else {
-            a.load_some(up + at, n);
-            b.load_some(from + at, n);
-        }
-        float v[N];
+    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        Piece<DT> a[U], b[U];
+        load<DT, W, false>(a, up, at, n);
+        load<DT, W, STREAMED>(b, from, at, n);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = w * a.get(i);
-            dot = __builtin_fmaf(a.get(i), b.get(i), dot);
+        for (int u = 0; u < U; ++u) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[i] = w * a[u].get(i);
+                dot = __builtin_fmaf(a[u].get(i), b[u].get(i), dot);
+            }
+            a[u].set(v);
         }
-        a.set(v);
-        if (n == N) a.store(to + at);
-        else a.store_some(to + at, n);
+        store<DT, W>(a, to, at, n);
     });
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
     if (lane == 0) dweights[id] = dot;
 }
 
+// Whether rows that are read once come by streaming loads: where they are much of what the last cache level keeps, in whole cache lines.  us, plain / streaming:
+// 16384 binary32 rows of 4096 gathered 108 / 82, combined 124 / 89; 16384 bf16 rows of 4096, two a token, combined 48 / 42, gradient 69 / 56; 8192 of these, four a
+// token, 20 / 22 and 27 / 27; 7108 binary32 rows of 1027, which share lines, combined 12.5 / 17.5.
+constexpr int64_t STREAM_MB = 96;
+static bool streams(const void *rows, int64_t n, int64_t cols, int dt)
+{
+    const int64_t row = cols * (dt == NVFP4_BF16 ? 2 : 4);
+    return row % 128 == 0 && reinterpret_cast<uintptr_t>(rows) % 128 == 0 && n * row >= ((int64_t)STREAM_MB << 20);
+}
+
 hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out,
                              hipStream_t st)
 {
-    auto *k = dt == NVFP4_BF16 ? moe_gather_kernel<NVFP4_BF16> : moe_gather_kernel<NVFP4_F32>;
+    const bool s = top_k == 1 && ld == cols && streams(x, x_rows, cols, dt);
+    auto *k = dt == NVFP4_BF16 ? (s ? moe_gather_kernel<NVFP4_BF16, true> : moe_gather_kernel<NVFP4_BF16, false>)
+                               : (s ? moe_gather_kernel<NVFP4_F32, true> : moe_gather_kernel<NVFP4_F32, false>);
     k<<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
                                                        reinterpret_cast<uint8_t *>(out));
     return hipGetLastError();
@@ -374,7 +429,9 @@ hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols
 hipError_t launch_moe_combine(const void *y, int dt, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position, int64_t tokens,
                               int32_t top_k, void *out, hipStream_t st)
 {
-    auto *k = dt == NVFP4_BF16 ? moe_combine_kernel<NVFP4_BF16> : moe_combine_kernel<NVFP4_F32>;
+    const bool s = streams(y, y_rows, cols, dt);
+    auto *k = dt == NVFP4_BF16 ? (s ? moe_combine_kernel<NVFP4_BF16, true> : moe_combine_kernel<NVFP4_BF16, false>)
+                               : (s ? moe_combine_kernel<NVFP4_F32, true> : moe_combine_kernel<NVFP4_F32, false>);
     k<<<dim3((unsigned)((tokens + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position, tokens, top_k,
                                                          reinterpret_cast<uint8_t *>(out));
     return hipGetLastError();
@@ -384,7 +441,9 @@ hipError_t launch_moe_combine_bwd(const void *dout, const void *y, int dt, int64
                                   const int32_t *kept, int64_t tokens, int32_t top_k, void *dy, float *dweights, hipStream_t st)
 {
     const int64_t pairs = tokens * top_k, clearing = rows < 256 ? rows : 256;
-    auto *k = dt == NVFP4_BF16 ? moe_combine_bwd_kernel<NVFP4_BF16> : moe_combine_bwd_kernel<NVFP4_F32>;
+    const bool s = streams(y, rows, cols, dt);
+    auto *k = dt == NVFP4_BF16 ? (s ? moe_combine_bwd_kernel<NVFP4_BF16, true> : moe_combine_bwd_kernel<NVFP4_BF16, false>)
+                               : (s ? moe_combine_bwd_kernel<NVFP4_F32, true> : moe_combine_bwd_kernel<NVFP4_F32, false>);
     k<<<dim3((unsigned)((pairs + clearing + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols,
                                                                    weights, position, kept, pairs, top_k, reinterpret_cast<uint8_t *>(dy), dweights);
     return hipGetLastError();
