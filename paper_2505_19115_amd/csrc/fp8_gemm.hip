@@ -131,9 +131,9 @@ constexpr double K_TILE_BF16 = 0.85, K_TILE_F32 = 2.2;
 template <int MODE>
 static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
 {
-    // Outputs past what the last cache level holds leave by streaming stores: 268 MB of weight gradients (8192 x 2 of 16, 4096 x 2048) 175 -> 155 us,
-    // but 90 MB (4096 x 11008 x 4096) 154 -> 160, 134 MB the same.
-    P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * 2 > ((int64_t)256 << 20);
+    // Outputs past what the last cache level holds leave by streaming stores: 256 MB of weight gradients (8192 x 2 of 16, 4096 x 2048) 175 -> 155 us,
+    // but 86 MB (4096 x 11008 x 4096) 154 -> 160, 128 MB the same.
+    P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * (out_dt == NVFP4_F32 ? 4 : 2) >= ((int64_t)256 << 20);
     const int64_t mine = f8g::tiles<MODE>(P, 128, 128), slots = 2 * compute_units();
     const double cost = (double)((mine + slots - 1) / slots) * (out_dt == NVFP4_F32 ? K_TILE_F32 : K_TILE_BF16);
     const double wide = P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE, out_dt) : 1e30;

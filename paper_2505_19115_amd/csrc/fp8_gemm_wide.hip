@@ -29,6 +29,10 @@ namespace nvfp4 {
 namespace f8w {
 
 constexpr int BM = 256, KT = FP8_BLOCK;
+// Weight gradients of so many tiles an expert are walked expert by expert, each over all XCDs (contractions differ in length as the tokens do); else an XCD takes a
+// band of the experts' tiles, whose operands its L2 then keeps.  us, band / each: 16 experts' 4096 x 2048 with 300 to 2281 of 16384 rows (128 tiles) 241 / 187; 64 experts'
+// 1024 x 1024 with 23 to 3016 of 32768 (24 tiles) 75 / 83.
+constexpr int SPREAD = 64;
 // FB: fragments of 16 columns of a wave; the workgroup's tile is 256 x 32 FB
 template <int FB, int OUT_DT>
 struct Geom {
@@ -128,14 +132,23 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             }
         }
         __syncthreads();
-        nty = MODE == FP8_EXPERTS ? __builtin_amdgcn_readfirstlane(group_tile[groups]) : nty * P.groups;
+        if (MODE == FP8_EXPERTS) nty = __builtin_amdgcn_readfirstlane(group_tile[groups]);
     }
     // An output without a contraction (rows of no expert, an expert without rows) is one K tile of whatever is there, stored as zeros: `keep` is a mask.
     auto find = [&](int id, uint32_t &keep) -> Tile {
         Tile T;
         keep = ~0u;
-        int ty, tx;
-        tile_coords(id, ntx, nty, ty, tx);
+        int ty, tx, e = 0;
+        if (MODE == FP8_EXPERTS_DW && ntx * nty >= f8w::SPREAD) {
+            e = id / (ntx * nty);
+            tile_coords(id - e * ntx * nty, ntx, nty, ty, tx);
+        } else {
+            tile_coords(id, ntx, MODE == FP8_EXPERTS_DW ? nty * P.groups : nty, ty, tx);
+            if (MODE == FP8_EXPERTS_DW) {
+                e = ty / nty;
+                ty -= e * nty;
+            }
+        }
         T.k0 = 0;
         T.count = P.blocks;
         T.b0 = T.out = 0;
@@ -143,7 +156,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         if constexpr (MODE == FP8_EXPERTS) {
             int n = 0;
             for (int e0 = 0; e0 <= P.groups; e0 += 64) n += __popcll(__ballot(e0 + lane <= P.groups && group_tile[e0 + lane <= P.groups ? e0 + lane : 0] <= ty));
-            const int e = __builtin_amdgcn_readfirstlane(n - 1);
+            e = __builtin_amdgcn_readfirstlane(n - 1);
             const int row = __builtin_amdgcn_readfirstlane(group_row[e] + (ty - group_tile[e]) * BM), end = __builtin_amdgcn_readfirstlane(group_row[e + 1]);
             T.m0 = row;
             left = end - row;
@@ -151,8 +164,6 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             else keep = 0;  // rows of no expert: zeros
         } else {
             if (MODE == FP8_EXPERTS_DW) {
-                const int per = nty / P.groups, e = ty / per;
-                ty -= e * per;
                 const int row = __builtin_amdgcn_readfirstlane(group_row[e]), rows = __builtin_amdgcn_readfirstlane(group_row[e + 1]) - row;
                 T.k0 = row / KT + e;
                 T.count = rows > 0 ? (rows + KT - 1) / KT : 1;
@@ -274,7 +285,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     __builtin_amdgcn_s_barrier(); \
     asm volatile("" ::: "memory");
 
-    const int tiles = ntx * nty;
+    const int tiles = ntx * nty * (MODE == FP8_EXPERTS_DW ? P.groups : 1);
     int id = (int)blockIdx.x;
     if (id >= tiles) return;
     uint32_t keep, next_keep = 0;

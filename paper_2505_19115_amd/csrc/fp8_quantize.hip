@@ -28,12 +28,13 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < W; ++i) w[i] = 0;
     }
+    template <bool STREAMED>
     __device__ __forceinline__ void load(const uint8_t *p)
     {
         struct __attribute__((packed, aligned(ESZ))) P { u32x4_t w; };
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
-            const u32x4_t v = reinterpret_cast<const P *>(p)[i].w;
+            const u32x4_t v = STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p) + i) : reinterpret_cast<const P *>(p)[i].w;
 #pragma unroll
             for (int k = 0; k < 4; ++k) w[4 * i + k] = v[k];
         }
@@ -105,7 +106,7 @@ __device__ __forceinline__ u32x2_t eight_codes(const Eight<DT> &x, float q)
 
 // Elements col .. col + 7 of N rows r0, r0 + step, ..., of which there are `have` (rows past these, and rows that an order does not name, are zeros).
 // Loads of whole pieces do not branch: a row that is not there reads the first one instead.
-template <int DT, int N>
+template <int DT, bool STREAMED, int N>
 __device__ __forceinline__ void load_rows(const Fp8QuantArgs &P, f8::Eight<DT> (&x)[N], int64_t r0, int have, int64_t col, bool whole)
 {
     constexpr int ESZ = f8::Eight<DT>::ESZ;
@@ -127,7 +128,7 @@ __device__ __forceinline__ void load_rows(const Fp8QuantArgs &P, f8::Eight<DT> (
     }
     if (whole) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i].load(base + (src[i] < 0 ? 0 : src[i]) * P.ld * ESZ);
+        for (int i = 0; i < N; ++i) x[i].template load<STREAMED>(base + (src[i] < 0 ? 0 : src[i]) * P.ld * ESZ);
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -137,7 +138,7 @@ __device__ __forceinline__ void load_rows(const Fp8QuantArgs &P, f8::Eight<DT> (
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (src[i] < 0 || left <= 0) x[i].zero();
-            else if (left >= 8) x[i].load(base + src[i] * P.ld * ESZ);
+            else if (left >= 8) x[i].template load<STREAMED>(base + src[i] * P.ld * ESZ);
             else x[i].load_some(base + src[i] * P.ld * ESZ, (int)left);
         }
     }
@@ -145,7 +146,7 @@ __device__ __forceinline__ void load_rows(const Fp8QuantArgs &P, f8::Eight<DT> (
 
 // Rows alone.  16 lanes hold a block, a wave four groups of RPG consecutive rows each: as many loads in flight, and their scale bytes are
 // neighbours in the block-major scales.
-template <int DT, int RPG>
+template <int DT, bool STREAMED, int RPG>
 __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs P, int64_t rows, int blocks, unsigned across)
 {
     using namespace f8;
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs P, 
     const int64_t r0 = ((int64_t)up * 4 + (lane >> 4)) * RPG;
     const int64_t col = (int64_t)kb * FP8_BLOCK + in * 8;
     Eight<DT> x[RPG];
-    load_rows<DT, RPG>(P, x, r0, (int)(rows - r0 < RPG ? rows - r0 : RPG), col, (int64_t)(kb + 1) * FP8_BLOCK <= P.cols);
+    load_rows<DT, STREAMED, RPG>(P, x, r0, (int)(rows - r0 < RPG ? rows - r0 : RPG), col, (int64_t)(kb + 1) * FP8_BLOCK <= P.cols);
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < RPG; ++i) {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs P, 
 
 // Columns, or both sides from one read: a workgroup takes 128 rows (a column block: of one matrix, or of one group of rows) by 128 columns,
 // a thread 8 rows by 8 columns of them, all in registers.  Codes of the column side turn through the LDS into rows of 128 bytes.
-template <int DT, bool ROWS>
+template <int DT, bool STREAMED, bool ROWS>
 __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, int col_tiles, int slots)
 {
     using namespace f8;
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
     if (count <= 0) return;
     const int64_t col = (int64_t)tile * FP8_BLOCK + cg * 8;
     Eight<DT> x[8];
-    load_rows<DT, 8>(P, x, row0 + rg * 8, count - rg * 8, col, (int64_t)(tile + 1) * FP8_BLOCK <= P.cols);
+    load_rows<DT, STREAMED, 8>(P, x, row0 + rg * 8, count - rg * 8, col, (int64_t)(tile + 1) * FP8_BLOCK <= P.cols);
     // columns' largest magnitudes: of the thread's rows, of the wave's, of all
 #pragma unroll
     for (int j = 0; j < Eight<DT>::W; ++j) {
@@ -259,25 +260,33 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
     }
 }
 
-hipError_t launch_fp8_quantize(const Fp8QuantArgs &P, int dt, hipStream_t st)
+template <int DT, bool STREAMED>
+static hipError_t launch(const Fp8QuantArgs &P, hipStream_t st)
 {
     const int64_t tiles = (P.cols + FP8_BLOCK - 1) / FP8_BLOCK;
     if (!P.codes_c) {
         const int64_t rows = P.batch * P.rows, across = (tiles + 3) / 4;
         // few rows: one a group of lanes, so that more waves load
-        const int rpg = rows * tiles >= 32 * 1024 ? 8 : 1;
+        const int rpg = STREAMED || rows * tiles >= 32 * 1024 ? 8 : 1;
         const dim3 grid((unsigned)(across * ((rows + 4 * rpg - 1) / (4 * rpg))));
-        auto *k = dt == NVFP4_BF16 ? (rpg == 8 ? fp8_quantize_rows_kernel<NVFP4_BF16, 8> : fp8_quantize_rows_kernel<NVFP4_BF16, 1>)
-                                   : (rpg == 8 ? fp8_quantize_rows_kernel<NVFP4_F32, 8> : fp8_quantize_rows_kernel<NVFP4_F32, 1>);
-        k<<<grid, 256, 0, st>>>(P, rows, (int)tiles, (unsigned)across);
+        if (rpg == 8) fp8_quantize_rows_kernel<DT, STREAMED, 8><<<grid, 256, 0, st>>>(P, rows, (int)tiles, (unsigned)across);
+        else fp8_quantize_rows_kernel<DT, false, 1><<<grid, 256, 0, st>>>(P, rows, (int)tiles, (unsigned)across);
         return hipGetLastError();
     }
     const int64_t slots = fp8_slots(P.rows, P.offsets ? P.groups : 0);
     const dim3 grid((unsigned)(tiles * slots * P.batch));
-    auto *k = dt == NVFP4_BF16 ? (P.codes_r ? fp8_quantize_tile_kernel<NVFP4_BF16, true> : fp8_quantize_tile_kernel<NVFP4_BF16, false>)
-                               : (P.codes_r ? fp8_quantize_tile_kernel<NVFP4_F32, true> : fp8_quantize_tile_kernel<NVFP4_F32, false>);
-    k<<<grid, 256, 0, st>>>(P, (int)tiles, (int)slots);
+    if (P.codes_r) fp8_quantize_tile_kernel<DT, STREAMED, true><<<grid, 256, 0, st>>>(P, (int)tiles, (int)slots);
+    else fp8_quantize_tile_kernel<DT, STREAMED, false><<<grid, 256, 0, st>>>(P, (int)tiles, (int)slots);
     return hipGetLastError();
+}
+
+hipError_t launch_fp8_quantize(const Fp8QuantArgs &P, int dt, hipStream_t st)
+{
+    // Tensors past what the last cache level holds come by streaming loads (they need 16-byte aligned rows).  us, both sides: 65536 x 2048 bf16 111 / 93, 16384 x 8192
+    // binary32 (rows) 126 / 116; 8192 x 8192 bf16 50 / 51, 4096 x 11008 binary32 49 / 58.
+    const int64_t esz = dt == NVFP4_BF16 ? 2 : 4;
+    const bool s = !P.order && P.ld * esz % 16 == 0 && reinterpret_cast<uintptr_t>(P.x) % 16 == 0 && P.batch * P.rows * P.cols * esz >= ((int64_t)256 << 20);
+    return dt == NVFP4_BF16 ? (s ? launch<NVFP4_BF16, true>(P, st) : launch<NVFP4_BF16, false>(P, st)) : s ? launch<NVFP4_F32, true>(P, st) : launch<NVFP4_F32, false>(P, st);
 }
 
 }  // namespace nvfp4
