@@ -74,7 +74,7 @@ struct Fp8GemmArgs {
 };
 // The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
 // few tiles; 256 rows by 128 to 256 columns (binary32 outputs: 128); 128 x 128.
-double fp8_gemm_thin_cost(const Fp8GemmArgs &P, int mode);
+double fp8_gemm_thin_cost(const Fp8GemmArgs &P);
 hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt);
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);

@@ -142,7 +142,7 @@ static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
     if (MODE == FP8_EXPERTS && P.M <= (out_dt == NVFP4_BF16 ? 8 : 16) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     if (MODE == FP8_DENSE) {
         // (expanding codes for binary32: 2000 x 2000 x 2000 44 / 34, 1056 x 2080 x 2784 36 / 43)
-        const double thin = fp8_gemm_thin_cost(P, MODE) * (out_dt == NVFP4_F32 ? 1.3 : 1.0);
+        const double thin = fp8_gemm_thin_cost(P) * (out_dt == NVFP4_F32 ? 1.3 : 1.0);
         if (thin < cost && thin < wide) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     }
     // A short contraction in few tiles: the larger ones take 1 to 2 us more to begin and end (experts 300 tokens, 3 of 10, 500 x 700 8.7 / 10.5, their weight

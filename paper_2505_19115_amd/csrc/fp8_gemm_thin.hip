@@ -6,7 +6,7 @@
 
 namespace nvfp4 {
 
-// MT, TN: fragments of 16 rows of A and of 16 columns.  U: K tiles of a batch.
+// MT, TN: fragments of 16 rows of A and of 16 columns.  U: K tiles of a batch (a wave without so many loads its last once more and does not multiply it).
 template <int MODE, int OUT_DT, int MT, int TN, int U, int NW>
 __global__ __launch_bounds__(64 * NW) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
 {
@@ -99,11 +99,20 @@ __global__ __launch_bounds__(64 * NW) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
 }
 
 template <int MODE, int MT, int TN, int U, int NW>
-static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+static hipError_t launch_batches(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     auto *k = out_dt == NVFP4_F32 ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, TN, U, NW> : fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, TN, U, NW>;
     k<<<dim3((unsigned)f8g::tiles<MODE>(P, 16 * MT, 16 * TN)), 64 * NW, 0, st>>>(P);
     return hipGetLastError();
+}
+
+// (batches of no more K tiles than a wave has: 64 experts of 1024 x 2048 with 2 tokens each, 16 K tiles, 64 us in batches of 4 by 8 waves, 30 by 4)
+template <int MODE, int MT, int TN, int U, int NW>
+static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+{
+    if (U >= 4 && P.blocks >= 4 * NW) return launch_batches<MODE, MT, TN, U, NW>(P, out_dt, st);
+    if (U >= 2 && P.blocks >= 2 * NW) return launch_batches<MODE, MT, TN, U < 2 ? U : 2, NW>(P, out_dt, st);
+    return launch_batches<MODE, MT, TN, 1, NW>(P, out_dt, st);
 }
 
 // Shapes of a workgroup's output: rows and columns in 16s.  What bounds these kernels is what a CU's loads bring, (MT + TN) * 16 rows of a K tile at 36 GB/s: the
@@ -115,21 +124,19 @@ struct Shape {
 constexpr Shape SHAPES[] = {{1, 1}, {1, 2}, {1, 3}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {4, 2}, {4, 3}, {4, 4}};
 constexpr double PER_16_ROWS = 0.057;  // us
 
-inline int64_t workgroups(const Fp8GemmArgs &P, int mode, Shape s)
+inline int64_t workgroups(const Fp8GemmArgs &P, Shape s)
 {
-    const int64_t rows = mode == FP8_EXPERTS ? (P.M < P.groups ? P.M : P.groups) + P.M / (16 * s.mt) : (P.M + 16 * s.mt - 1) / (16 * s.mt);
-    return rows * ((P.N + 16 * s.tn - 1) / (16 * s.tn));
+    return (P.M + 16 * s.mt - 1) / (16 * s.mt) * ((P.N + 16 * s.tn - 1) / (16 * s.tn));
 }
 }  // namespace f8t
 
-static f8t::Shape shape_of(const Fp8GemmArgs &P, int mode, double *cost)
+static f8t::Shape shape_of(const Fp8GemmArgs &P, double *cost)
 {
     const int64_t cus = compute_units();
     f8t::Shape best = f8t::SHAPES[0];
     *cost = 1e30;
     for (const f8t::Shape s : f8t::SHAPES) {
-        if (mode == FP8_EXPERTS && s.mt > 1) continue;
-        const double c = (double)((f8t::workgroups(P, mode, s) + cus - 1) / cus) * (s.mt + s.tn) * f8t::PER_16_ROWS;
+        const double c = (double)((f8t::workgroups(P, s) + cus - 1) / cus) * (s.mt + s.tn) * f8t::PER_16_ROWS;
         if (c < *cost) {
             *cost = c;
             best = s;
@@ -138,10 +145,10 @@ static f8t::Shape shape_of(const Fp8GemmArgs &P, int mode, double *cost)
     return best;
 }
 
-double fp8_gemm_thin_cost(const Fp8GemmArgs &P, int mode)
+double fp8_gemm_thin_cost(const Fp8GemmArgs &P)
 {
     double cost;
-    shape_of(P, mode, &cost);
+    shape_of(P, &cost);
     return cost;
 }
 
@@ -149,7 +156,7 @@ hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, 
 {
     if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, 1, 2, 4, 4>(P, out_dt, st);
     double cost;
-    const f8t::Shape s = shape_of(P, mode, &cost);
+    const f8t::Shape s = shape_of(P, &cost);
     switch (4 * s.mt + s.tn) {
     case 5: return launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st);
     case 6: return launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st);
