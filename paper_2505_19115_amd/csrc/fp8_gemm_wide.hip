@@ -384,8 +384,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             using Frags = std::integral_constant<int, 8>;
             quarter(I0{}, HP{}, [&](auto j) {
                 if constexpr (decltype(j)::value < 2 * HB) read_b(ST, HB * (1 - ST) + (decltype(j)::value >> 1), decltype(j)::value & 1);
-                spread(j, std::integral_constant<int, 4 * HB - (G::FIRST < 3 * HB ? G::FIRST : 3 * HB)>{}, std::integral_constant<int, G::FIRST>{},
-                       [&](auto i) { request_first(stage, i); });
+                spread(j, F0{}, std::integral_constant<int, G::FIRST>{}, [&](auto i) { request_first(stage, i); });
             });
             quarter(I0{}, HQ{}, [&](auto j) { spread(j, F0{}, Frags{}, [&](auto i) { read_a(ST, 4 + (decltype(i)::value >> 1), decltype(i)::value & 1); }); });
             NVFP4_F8W_WAIT(ALL)
@@ -393,7 +392,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             __builtin_amdgcn_sched_barrier(0);
             quarter(I1{}, HQ{}, [&](auto j) {
                 spread(j, F0{}, Frags{}, [&](auto i) { read_a(1 - ST, decltype(i)::value >> 1, decltype(i)::value & 1); });
-                spread(j, FH{}, std::integral_constant<int, G::SECOND>{}, [&](auto i) { request_second(stage, i); });
+                spread(j, F0{}, std::integral_constant<int, G::SECOND>{}, [&](auto i) { request_second(stage, i); });
             });
             advance();
             quarter(I1{}, HP{}, [&](auto j) {

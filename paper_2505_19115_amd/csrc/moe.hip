@@ -14,6 +14,7 @@ namespace nvfp4 {
 namespace moe {
 
 constexpr int WAVES = 16, NT = 64 * WAVES;
+constexpr int AHEAD = 4;  // loads of pairs' experts in flight: one after the other, four of them took half of the time
 
 // Exclusive prefix sum of one value per thread over the workgroup; *total receives the sum
 __device__ __forceinline__ int prefix(int v, int *per_wave, int *total)
@@ -58,9 +59,13 @@ __global__ __launch_bounds__(1024) void moe_count_kernel(const ID *ids, int64_t 
     for (int e = threadIdx.x; e < groups; e += NT) hist[e] = 0;
     __syncthreads();
     const int64_t first = blockIdx.x * part, last = first + part < n ? first + part : n;
-    for (int64_t i = first + threadIdx.x; i < last; i += NT) {
-        const int e = expert_of(ids, i, last, groups);
-        if (e >= 0) atomicAdd(&hist[e], 1);
+    for (int64_t i = first + threadIdx.x; i < last; i += AHEAD * NT) {
+        int e[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) e[u] = expert_of(ids, i + u * NT, last, groups);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (e[u] >= 0) atomicAdd(&hist[e[u]], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < groups; e += NT) counts[(int64_t)blockIdx.x * groups + e] = hist[e];
@@ -81,9 +86,17 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(const ID *ids, int64_t 
     int *const mine = hist + wave * groups;
     for (int i = tid; i < WAVES * groups; i += NT) hist[i] = 0;
     __syncthreads();
-    for (int64_t i = w0 + lane; i < w1; i += 64) {
-        const int e = expert_of(ids, i, w1, groups);
-        if (e >= 0) atomicAdd(&mine[e], 1);
+    int own[AHEAD];  // the wave's first 64 AHEAD pairs, which are placed from here
+    for (int64_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
+        int e[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            e[u] = expert_of(ids, i0 + u * 64 + lane, w1, groups);
+            if (i0 == w0) own[u] = e[u];
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (e[u] >= 0) atomicAdd(&mine[e[u]], 1);
     }
     __syncthreads();
     // thread e: the expert's pairs of all parts, of the parts before this one, of the waves before each (groups <= NT).  The counts of many parts are
@@ -129,22 +142,29 @@ __global__ __launch_bounds__(1024) void moe_place_kernel(const ID *ids, int64_t 
     if (blockIdx.x == 0 && tid == 0) offsets[groups] = total;
     __syncthreads();
     const int bits = 32 - __builtin_clz((unsigned)groups);
-    for (int64_t i0 = w0; i0 < w1; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const int e = expert_of(ids, i, w1, groups);
-        uint64_t same = __ballot(e >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t ones = __ballot((e >> b) & 1);
-            same &= (e >> b) & 1 ? ones : ~ones;
-        }
-        if (e >= 0) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int slot = *const_cast<volatile int *>(&mine[e]) + rank;
-            if (rank == 0) atomicAdd(&mine[e], __popcll(same));  // (behind the wave's reads: LDS accesses of a wave keep their order)
-            order[slot] = (int32_t)i;
-            position[i] = slot;
-        } else if (i < w1) {
-            position[i] = -1;
+    for (int64_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
+        int expert[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) expert[u] = i0 == w0 ? own[u] : expert_of(ids, i0 + u * 64 + lane, w1, groups);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t i = i0 + u * 64 + lane;
+            if (i0 + u * 64 >= w1) break;
+            const int e = expert[u];
+            uint64_t same = __ballot(e >= 0);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t ones = __ballot((e >> b) & 1);
+                same &= (e >> b) & 1 ? ones : ~ones;
+            }
+            if (e >= 0) {
+                const int rank = __popcll(same & ((1ull << lane) - 1));
+                const int slot = *const_cast<volatile int *>(&mine[e]) + rank;
+                if (rank == 0) atomicAdd(&mine[e], __popcll(same));  // (behind the wave's reads: LDS accesses of a wave keep their order)
+                order[slot] = (int32_t)i;
+                position[i] = slot;
+            } else if (i < w1) {
+                position[i] = -1;
+            }
         }
     }
     for (int64_t i = first + tid; i < last; i += NT)
