@@ -1,7 +1,7 @@
 // Products of quantized 8-bit operands ("NT": both stored with the contraction axis contiguous),
 //     out[i, j] = sum_b 2^(sA[b,i] - 127) 2^(sB[b,j] - 127) sum_{k in b} cA[i,k] cB[j,k],
 // on v_mfma_scale_f32_16x16x128_f8f6f4, which takes 128 contraction elements of 16 rows of each operand with the rows' scale bytes: one
-// instruction is one block, and the scales cost nothing.  Products of codes are exact, sums are binary32.
+// instruction is one block, and the scales cost nothing.  What its sums lose, and what binary32 outputs take in its place: fp8_gemm.h.
 //
 // One body serves the dense product, the experts' (rows of A divided among weights) and the experts' weight gradients (a contraction
 // divided among outputs): they differ in which rows and K tiles a workgroup's tile covers (Tile).
