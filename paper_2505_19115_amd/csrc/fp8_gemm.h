@@ -1,5 +1,6 @@
 // What the kernels of 8-bit products share: which rows and K tiles a workgroup's tile covers, scale bytes, fragments, and the way out.
 #pragma once
+#include <type_traits>
 #include "experts.h"
 #include "kernels.h"
 
@@ -197,41 +198,32 @@ __device__ __forceinline__ void store_four(void *out, int64_t at, const float4v_
     }
 }
 
-// n of four columns of one row, in binary32
-template <bool STREAMED>
-__device__ __forceinline__ void store_words(void *out, int64_t at, const u32x4_t &w, int n)
+__device__ __forceinline__ u32x4_t to_bf16(const float (&v)[8])
 {
-    typedef u32x4_t __attribute__((aligned(4))) anywhere_t;
-    uint32_t *const p = reinterpret_cast<uint32_t *>(out) + at;
-    if (n >= 4) {
-        if (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<anywhere_t *>(p));
-        else *reinterpret_cast<anywhere_t *>(p) = w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < n) p[i] = w[i];
-    }
-}
-
-// n of eight columns of one row, in bf16, masked
-template <bool STREAMED>
-__device__ __forceinline__ void store_eight(void *out, int64_t at, const float (&v)[8], int n, uint32_t keep)
-{
-    typedef u32x4_t __attribute__((aligned(2))) anywhere_t;
-    uint16_t *const p = reinterpret_cast<uint16_t *>(out) + at;
     u32x4_t w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2v_t f = {v[2 * i], v[2 * i + 1]};
-        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t)) & keep;
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
     }
-    if (n >= 8) {
+    return w;
+}
+
+// n of the four (binary32) or eight (bf16) columns of one row that fill 16 bytes
+template <int OUT_DT, bool STREAMED>
+__device__ __forceinline__ void store_lane(void *out, int64_t at, const u32x4_t &w, int n)
+{
+    typedef std::conditional_t<OUT_DT == NVFP4_F32, uint32_t, uint16_t> element_t;
+    typedef u32x4_t __attribute__((aligned(2))) anywhere_t;
+    constexpr int N = 16 / sizeof(element_t);
+    element_t *const p = reinterpret_cast<element_t *>(out) + at;
+    if (n >= N) {
         if (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<anywhere_t *>(p));
         else *reinterpret_cast<anywhere_t *>(p) = w;
     } else {
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        for (int i = 0; i < N - 1; ++i)
+            if (i < n) p[i] = (element_t)(w[i * 4 / N] >> (N == 8 ? 16 * (i & 1) : 0));
     }
 }
 

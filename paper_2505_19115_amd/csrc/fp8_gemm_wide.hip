@@ -4,7 +4,7 @@
 //
 // LDS: two stages of one K tile, 32 KB of each operand, 16 positions a fragment; chunk h of position 16 f + c at slot h ^ (c / 2), and lane (c, q) reads chunks
 // q and q + 4 (fp8_gemm.hip).  A's rows stand in their order; B's so that a lane ends with eight neighbouring columns and its three neighbours with those
-// beside them, one store of 64 bytes a row: fragment 2 s + h of 64 columns has the columns 32 s + 8 (c / 4) + 4 h + c % 4.  Beside them the 512 scale
+// beside them, 64 bytes a row: fragment 2 s + h of 64 columns has the columns 32 s + 8 (c / 4) + 4 h + c % 4.  Beside them the 512 scale
 // bytes, a dword each, four fragments' of a lane together.  All of it is written by direct global ->
 // LDS loads (scales byte by byte: they start anywhere), so that the loads in flight can be counted.  Rows past the edge are clamped to the last one.
 //
@@ -18,8 +18,13 @@
 // the counts hold.
 //
 // Workgroups stay (one per CU) and walk the output tiles: the first two K tiles of the next one are requested before this one's outputs are
-// stored.  Which tiles there are for how many rows of an expert is
-// counted once, into the LDS.
+// stored.  Stores are of whole lines, eight rows' at a time, for which lanes eight apart exchange halves: a CU takes a tile's 128 KB in 5000 cycles so, in 8000
+// by stores of sixteen half lines (8192 x 8192 x 1024 80.2 -> 78.6 us, 16 experts' weight gradients 4096 x 2048 from 16384 rows 155 -> 150).  Which tiles there are
+// for how many rows of an expert is counted once, into the LDS.
+//
+// What bounds it: long contractions the matrix instructions (4096 x 4096 x 11008 127 us, 2.9 PFLOP/s, 2290 cycles a K tile of which 2048 are MFMAs; 8192^3 360 us, 3.05
+// PFLOP/s; the power limit lowers the clock to 2 GHz), short ones what is not them: of 8192 x 8192 x 1024 (79 us, 1.7 PFLOP/s) a tile takes 35000 cycles, 23000 for
+// eight K tiles, of which the first wait for memory, 8000 for the stores, which all CUs do at once, 3000 to find and request the next tile.
 #include <atomic>
 #include <type_traits>
 
@@ -43,11 +48,26 @@ struct Geom {
     static constexpr int STORES = (OUT_DT == NVFP4_F32 ? 8 : 4) * FB;  // of a wave, for an output inside
 };
 
-// Column (of the wave's) that position c of fragment f holds: a lane ends with columns of one row that fill 16 bytes
-template <int OUT_DT>
-__device__ __forceinline__ int column(int f, int c)
+// Column of the tile that position c of fragment f of the waves `part` holds: a lane ends with columns of one row that fill 16 bytes.  Waves have whole
+// lines of the output, of 96 columns all but the last 32.
+template <int FB>
+__device__ __forceinline__ int columns_of(int part, int f)
 {
-    return OUT_DT == NVFP4_F32 ? 16 * f + c : 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3);
+    return FB == 6 && f >= 4 ? 128 + 32 * part : 16 * (FB == 6 ? 4 : FB) * part;
+}
+template <int OUT_DT, int FB>
+__device__ __forceinline__ int column(int part, int f, int c)
+{
+    return columns_of<FB>(part, f) + (FB == 6 && f >= 4 ? -64 : 0) + (OUT_DT == NVFP4_F32 ? 16 * f + c : 32 * (f >> 1) + 8 * (c >> 2) + 4 * (f & 1) + (c & 3));
+}
+
+// x of the lanes c < 8 and y of c + 8 in the others; and y of the lanes c >= 8, x of c + 8 in the others: of two halves of 16 rows' lines, the lines of eight rows each
+__device__ __forceinline__ void exchange(uint32_t &x, uint32_t &y)
+{
+    constexpr int ROTATE_8 = 0x128;
+    const uint32_t t = __builtin_amdgcn_update_dpp(x, y, ROTATE_8, 0xf, 0xc, false);
+    y = __builtin_amdgcn_update_dpp(y, x, ROTATE_8, 0xf, 0x3, false);
+    x = t;
 }
 
 // As assembly, so that the 64 accumulators stay where they are (gemm_mx.hip).  What the compiler does not know about it: an operand must not have been
@@ -199,11 +219,11 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
         }
 #pragma unroll
         for (int i = 0; i < FB; ++i) {
-            const int in = 16 * HB * (i / HB) + 8 * HB * side + 8 * (i % HB) + (lane >> 3), col = 16 * FB * part + f8w::column<OUT_DT>(in >> 4, in & 15);
+            const int in = 16 * HB * (i / HB) + 8 * HB * side + 8 * (i % HB) + (lane >> 3), col = f8w::column<OUT_DT, FB>(part, in >> 4, in & 15);
             offB[i] = (uint32_t)((col < T.cols ? col : T.cols - 1) * pitch) + ((lane & 7) ^ ((in & 15) >> 1)) * 16;
         }
         // dword 4 c + f of the wave's 64: position c of fragment 4 side + f of a part (of B those there are)
-        const int f = 4 * side + (lane & 3), row = 128 * part + 16 * f + (lane >> 2), col = 16 * FB * part + f8w::column<OUT_DT>(f < FB ? f : FB - 1, lane >> 2);
+        const int f = 4 * side + (lane & 3), row = 128 * part + 16 * f + (lane >> 2), col = f8w::column<OUT_DT, FB>(part, f < FB ? f : FB - 1, lane >> 2);
         offSA = row < T.rows ? row : T.rows - 1;
         offSB = col < T.cols ? col : T.cols - 1;
         pA = uniform(P.A + T.m0 * pitch + (int64_t)T.k0 * KT);
@@ -435,29 +455,44 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             int at_lane = lane;
             asm volatile("" : "+v"(at_lane));  // (or the addresses are computed before the K loop and kept)
             const int c = at_lane & 15, q = at_lane >> 4;
+            constexpr bool IN = decltype(inside)::value != 0, STREAMED = decltype(streamed)::value != 0;
+            // words of row 16 a + c that fill 64 bytes in four lanes (bf16: fragments 2 s and 2 s + 1; binary32: fragment s)
+            auto words = [&](int a, int s) -> u32x4_t {
+                if constexpr (OUT_DT == NVFP4_F32) return __builtin_bit_cast(u32x4_t, acc[a][s]) & keep;
+                float v[8];
+                // (reads that stay behind the wait states and leave the accumulators alone)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
+                return to_bf16(v) & keep;
+            };
+            constexpr int EACH = OUT_DT == NVFP4_F32 ? 16 : 32, N = 16 * FB / EACH;  // columns of such 64 bytes; how many
 #pragma unroll
             for (int a = 0; a < 8; ++a) {
-                if constexpr (OUT_DT == NVFP4_F32) {
+                const int64_t top = T.out + T.m0 + wm * 128 + 16 * a;
+                auto col_of = [&](int s) { return f8w::columns_of<FB>(wn, s * EACH / 16) + (FB == 6 && s * EACH >= 64 ? s * EACH - 64 : s * EACH); };
+                auto one = [&](int s) {
+                    const int row = wm * 128 + 16 * a + c, col = col_of(s) + q * (EACH / 4);
+                    const u32x4_t w = words(a, s);
+                    if (IN || (row < T.rows && col < T.cols)) store_lane<OUT_DT, STREAMED>(P.out, (top + c) * P.ldc + T.n0 + col, w, IN ? 16 : T.cols - col);
+                };
 #pragma unroll
-                    for (int b = 0; b < FB; ++b) {
-                        const int row = wm * 128 + 16 * a + c, col = wn * 16 * FB + 16 * b + 4 * q;
-                        const u32x4_t w = __builtin_bit_cast(u32x4_t, acc[a][b]) & keep;
-                        const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + col;
-                        if constexpr (decltype(inside)::value != 0) store_words<(decltype(streamed)::value != 0)>(P.out, at, w, 4);
-                        else if (row < T.rows && col < T.cols) store_words<false>(P.out, at, w, T.cols - col);
+                for (int s = 0; s < N; s += 2) {
+                    if (!IN || s + 1 == N) {
+                        one(s);
+                        if (s + 1 < N) one(s + 1);
+                        continue;
                     }
-                    continue;
-                }
+                    u32x4_t w = words(a, s), x = words(a, s + 1);
 #pragma unroll
-                for (int s = 0; s < HB; ++s) {
-                    const int row = wm * 128 + 16 * a + c, col = wn * 16 * FB + 32 * s + 8 * q;
-                    float v[8];
-                    // (reads that stay behind the wait states and leave the accumulators alone)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
-                    const int64_t at = (T.out + T.m0 + row) * P.ldc + T.n0 + col;
-                    if constexpr (decltype(inside)::value != 0) store_eight<(decltype(streamed)::value != 0)>(P.out, at, v, 8, keep);
-                    else if (row < T.rows && col < T.cols) store_eight<false>(P.out, at, v, T.cols - col, keep);
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t lo = w[i], hi = x[i];
+                        f8w::exchange(lo, hi);
+                        w[i] = lo;
+                        x[i] = hi;
+                    }
+                    const int64_t at = (top + (c & 7)) * P.ldc + T.n0 + col_of(s) + (c >> 3) * EACH + q * (EACH / 4);
+                    store_lane<OUT_DT, STREAMED>(P.out, at, w, 16);
+                    store_lane<OUT_DT, STREAMED>(P.out, at + 8 * P.ldc, x, 16);
                 }
             }
             NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
