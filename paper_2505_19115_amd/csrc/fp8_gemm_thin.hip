@@ -2,6 +2,10 @@
 // once and does little else, so nothing is staged: a workgroup has 16 columns and up to 64 rows, its waves divide the K tiles (wave w takes w, w + NW, ...), and
 // every lane loads its own codes, 32 of a row and K tile, a batch of K tiles at a time.  The waves' sums are added through the LDS
 // in the waves' order.
+//
+// What bounds it: loads in flight, and the first of them, which an expert's product asks for behind its offsets.  16 x 11008 x 4096 11.4 us, 4.0 TB/s; 16 x 16384 x
+// 4096 15.5 us, 4.4 TB/s; 8 experts of 2048 x 4096, 16 rows 17.3 us, 3.9 TB/s; a token's 2 of them 7.0 us, where one 4096 x 4096 takes 5.1.  Without effect: lanes that load
+// whole lines; slower: streaming loads (16 x 11008 x 4096 12.8 us), the experts' products on more columns (20 us) or more waves (20 us).
 #include "fp8_gemm.h"
 
 namespace nvfp4 {
@@ -116,12 +120,12 @@ static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 }
 
 // Shapes of a workgroup's output: rows and columns in 16s.  What bounds these kernels is what a CU's loads bring, (MT + TN) * 16 rows of a K tile at 36 GB/s: the
-// fewest rounds of the CUs times that.
+// fewest rounds of the CUs times that.  us, 16 rows, 48 columns at most / 64: 16384 x 4096 18.3 / 15.5, 28672 x 4096 32.5 / 28.3, 12288 x 4096 13.0 / 12.1.
 namespace f8t {
 struct Shape {
     int mt, tn;
 };
-constexpr Shape SHAPES[] = {{1, 1}, {1, 2}, {1, 3}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {4, 2}, {4, 3}, {4, 4}};
+constexpr Shape SHAPES[] = {{1, 1}, {1, 2}, {1, 3}, {1, 4}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {4, 2}, {4, 3}, {4, 4}};
 constexpr double PER_16_ROWS = 0.057;  // us
 
 inline int64_t workgroups(const Fp8GemmArgs &P, Shape s)
@@ -161,6 +165,7 @@ hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, 
     case 5: return launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st);
     case 6: return launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st);
     case 7: return launch_thin<FP8_DENSE, 1, 3, 4, 8>(P, out_dt, st);
+    case 8: return launch_thin<FP8_DENSE, 1, 4, 4, 8>(P, out_dt, st);
     case 9: return launch_thin<FP8_DENSE, 2, 1, 4, 8>(P, out_dt, st);
     case 10: return launch_thin<FP8_DENSE, 2, 2, 2, 8>(P, out_dt, st);
     case 11: return launch_thin<FP8_DENSE, 2, 3, 2, 8>(P, out_dt, st);

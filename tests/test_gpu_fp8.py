@@ -387,6 +387,18 @@ def test_experts(T, k, E, N, K, drop, only, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M, N, K", [(1, 16384, 300), (9, 16001, 700), (16, 13000, 129), (3, 30000, 5000)])
+def test_few_rows_of_many_columns(M, N, K, dtype):
+    g = torch.Generator().manual_seed(M + N + K)
+    a, b = (nv.fp8_quantize(tensor(g, n, K).cuda())[0] for n in (M, N))
+    out = nv.fp8_gemm(a, b, out_dtype=dtype)
+    A, B = values_on_gpu(a), values_on_gpu(b)
+    ref = A @ B.t()
+    most = A.abs() @ B.abs().t() * lost(A.shape[1], dtype) + (0 if dtype == torch.float32 else ROUNDED) * ref.abs() + 1e-300
+    assert bool(((out.double() - ref).abs() <= most).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_experts_large_tiles(dtype):
     # outputs of more tiles than CUs, uneven experts, weight gradients of many and of few tiles an expert
     g = torch.Generator().manual_seed(20)
