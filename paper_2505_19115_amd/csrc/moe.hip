@@ -5,7 +5,10 @@
 //   gather        out[slot] = x[order[slot] / top_k]
 //   combine       out[t] = sum_j w[t, j] y[position[t, j]], choices in their order, binary32
 //   combine_bwd   dy[position[t, j]] = w[t, j] dout[t],  dw[t, j] = sum_d dout[t, d] y[position[t, j], d]
-// All of it is bound by memory; a wave moves a row (of a pair, or of a token with its choices) in pieces of 16 bytes a lane.
+// What bounds rows is memory, at what a copy reaches (5.3 TB/s): a wave moves a row (of a pair, or of a token with its choices) in pieces of 16 bytes a lane.
+// 8192 tokens x 2 of 4096 bf16, combined 39.6 us (5.1 TB/s), gradient 52 to 62 (5.4 to 6.4, by what the last cache level still holds); 1777 x 4 of 1027 binary32
+// gathered 9.7 (3.8 TB/s: rows that share lines).  The sort is bound by latency: 32 pairs of 8 experts 3.3 us in one workgroup, 262144 of 128 experts 3.2 + 9.3
+// in 64 of them (128 and 256 the same), where its 4 MB take 0.8.
 #include <type_traits>
 
 #include "experts.h"
