@@ -472,6 +472,14 @@ nvfp4_status nvfp4_fp8_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *A_co
                             const uint8_t *B_codes, const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc,
                             void *stream);
 /*
+ * The same with scratch memory (16-byte aligned; as many bytes as the query says, which may be 0): an output of few tiles has its
+ * contraction divided among workgroups, whose binary32 sums meet there and are added in their order.
+ */
+size_t nvfp4_fp8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, nvfp4_dtype out_dt);
+nvfp4_status nvfp4_fp8_gemm_ws(int64_t M, int64_t N, int64_t K, const uint8_t *A_codes, const uint8_t *A_scales,
+                               const uint8_t *B_codes, const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc,
+                               void *workspace, size_t workspace_bytes, void *stream);
+/*
  * The experts' products.  A [rows, K] holds the gathered tokens in the experts' order, offsets (device int32
  * [groups + 1], ascending, 0 .. rows) says which are whose, B is an operand of groups * N rows, expert e's N from e N on:
  *   out[r, :] = A[r, :] B_e^T     for offsets[e] <= r < offsets[e + 1]; zeros for rows of no expert.

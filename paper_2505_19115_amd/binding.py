@@ -167,6 +167,10 @@ def _load() -> C.CDLL:
     L.nvfp4_fp8_quantize.argtypes = [vp, ci, i64, i64, i64, i64, vp, i32, i64, vp, i32, vp, vp, vp, vp, vp]
     L.nvfp4_fp8_gemm.restype = ci
     L.nvfp4_fp8_gemm.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, ci, i64, vp]
+    L.nvfp4_fp8_gemm_workspace_bytes.restype = sz
+    L.nvfp4_fp8_gemm_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    L.nvfp4_fp8_gemm_ws.restype = ci
+    L.nvfp4_fp8_gemm_ws.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, ci, i64, vp, sz, vp]
     L.nvfp4_fp8_gemm_experts.restype = L.nvfp4_fp8_gemm_experts_dw.restype = ci
     L.nvfp4_fp8_gemm_experts.argtypes = L.nvfp4_fp8_gemm_experts_dw.argtypes = [i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, ci, i64, vp]
     L.nvfp4_moe_sort_workspace_bytes.argtypes = [i64, i32]
@@ -213,7 +217,7 @@ EXPORTS = (
     "nvfp4_quant_noise_workspace_bytes", "nvfp4_quant_noise", "nvfp4_quantize_static", "nvfp4_cross_check_switches",
     "nvfp4_weight_operands_bytes", "nvfp4_quantize_weight", "nvfp4_linear_fwd_wq", "nvfp4_linear_bwd_wq",
     "nvfp4_swiglu_bwd_workspace_bytes", "nvfp4_swiglu_bwd_quantize", "nvfp4_linear_bwd_dyq", "nvfp4_host_swiglu_bwd", "nvfp4_swiglu_bwd",
-    "nvfp4_fp8_codes_bytes", "nvfp4_fp8_scales_bytes", "nvfp4_fp8_slots", "nvfp4_fp8_quantize", "nvfp4_fp8_gemm", "nvfp4_fp8_gemm_experts",
+    "nvfp4_fp8_codes_bytes", "nvfp4_fp8_scales_bytes", "nvfp4_fp8_slots", "nvfp4_fp8_quantize", "nvfp4_fp8_gemm", "nvfp4_fp8_gemm_workspace_bytes", "nvfp4_fp8_gemm_ws", "nvfp4_fp8_gemm_experts",
     "nvfp4_fp8_gemm_experts_dw", "nvfp4_moe_sort_workspace_bytes", "nvfp4_moe_sort", "nvfp4_moe_gather", "nvfp4_moe_combine", "nvfp4_moe_combine_bwd",
 )
 
@@ -776,7 +780,7 @@ def fp8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, order: 
 
 
 def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
-    """nvfp4_fp8_gemm: operands [M, K] and [N, K] -> [M, N]."""
+    """nvfp4_fp8_gemm_ws: operands [M, K] and [N, K] -> [M, N]."""
     (M, K), (N, Kb) = a.codes.shape, b.codes.shape
     if K != Kb:
         raise ValueError(f"contractions of {K} and {Kb}")
@@ -787,10 +791,18 @@ def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch
         if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
             raise ValueError(f"out: [{M}, {N}] in rows of neighbouring elements")
         ldc = out.stride(0) if M > 1 else N
-    code = lib.nvfp4_fp8_gemm(M, N, K, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), out.data_ptr(), _dtype_tag(out), ldc,
-                              _stream())
+    stream, tag = _stream(), _dtype_tag(out)
+    key = ("fp8_gemm", M, N, K, tag)
+    ws_bytes = _known_sizes.get(key)
+    if ws_bytes is None:
+        if len(_known_sizes) >= 1000:
+            _known_sizes.clear()
+        ws_bytes = _known_sizes[key] = lib.nvfp4_fp8_gemm_workspace_bytes(M, N, K, tag)
+    block = _Block(ws_bytes, out, stream) if ws_bytes else None
+    code = lib.nvfp4_fp8_gemm_ws(M, N, K, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), out.data_ptr(), tag, ldc,
+                                 block.ptr if block else None, ws_bytes, stream)
     if code:
-        _check(code, "nvfp4_fp8_gemm")
+        _check(code, "nvfp4_fp8_gemm_ws")
     return out
 
 

@@ -79,7 +79,7 @@ nvfp4_status nvfp4_fp8_quantize(const void *x, nvfp4_dtype dt_, int64_t batch, i
 }
 
 static nvfp4_status product(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32_t groups, const int32_t *offsets, int64_t total, const uint8_t *A_codes,
-                            const uint8_t *A_scales, const uint8_t *B_codes, const uint8_t *B_scales, void *out, int out_dt, int64_t ldc, void *stream)
+                            const uint8_t *A_scales, const uint8_t *B_codes, const uint8_t *B_scales, void *out, int out_dt, int64_t ldc, void *workspace, void *stream)
 {
     if (!valid_dtype(out_dt)) return NVFP4_EINVAL;
     if (M < 0 || N < 0 || K < 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || ldc < N || M > MOST_ROWS || N > MOST_ROWS) return NVFP4_ESHAPE;
@@ -106,6 +106,7 @@ static nvfp4_status product(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32
     P.offsets = offsets;
     P.groups = mode == FP8_DENSE ? 0 : groups;
     P.total = (int32_t)total;
+    P.partial = reinterpret_cast<float *>(workspace);
     if ((ceil_div(M, 16) + groups + 1) * ceil_div(N, 16) > MOST_GRID / (mode == FP8_EXPERTS_DW ? groups : 1)) return NVFP4_ESHAPE;
     return done(launch_fp8_gemm(P, mode, out_dt, reinterpret_cast<hipStream_t>(stream)));
 }
@@ -114,14 +115,34 @@ nvfp4_status nvfp4_fp8_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *A_co
                             const uint8_t *B_codes, const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc,
                             void *stream)
 {
-    return product(FP8_DENSE, M, N, K, 0, nullptr, 0, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc, stream);
+    return product(FP8_DENSE, M, N, K, 0, nullptr, 0, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc, nullptr, stream);
+}
+
+size_t nvfp4_fp8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, nvfp4_dtype out_dt)
+{
+    if (!valid_dtype(raw(out_dt)) || M <= 0 || N <= 0 || K <= 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || M > MOST_ROWS || N > MOST_ROWS) return 0;
+    Fp8GemmArgs P = {};
+    P.M = M;
+    P.N = N;
+    P.blocks = (int32_t)(K / FP8_BLOCK);
+    return fp8_gemm_workspace(P, raw(out_dt));
+}
+
+nvfp4_status nvfp4_fp8_gemm_ws(int64_t M, int64_t N, int64_t K, const uint8_t *A_codes, const uint8_t *A_scales,
+                               const uint8_t *B_codes, const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    const size_t need = nvfp4_fp8_gemm_workspace_bytes(M, N, K, out_dt);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return NVFP4_EWORKSPACE;
+    if (need > 0 && !aligned(workspace, 16)) return NVFP4_EALIGN;
+    return product(FP8_DENSE, M, N, K, 0, nullptr, 0, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc, need > 0 ? workspace : nullptr, stream);
 }
 
 nvfp4_status nvfp4_fp8_gemm_experts(int64_t rows, int64_t N, int64_t K, int32_t groups, const int32_t *offsets,
                                     const uint8_t *A_codes, const uint8_t *A_scales, const uint8_t *B_codes,
                                     const uint8_t *B_scales, void *out, nvfp4_dtype out_dt, int64_t ldc, void *stream)
 {
-    return product(FP8_EXPERTS, rows, N, K, groups, offsets, rows, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc, stream);
+    return product(FP8_EXPERTS, rows, N, K, groups, offsets, rows, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc, nullptr, stream);
 }
 
 nvfp4_status nvfp4_fp8_gemm_experts_dw(int64_t M, int64_t N, int64_t rows, int32_t groups, const int32_t *offsets,
@@ -131,7 +152,7 @@ nvfp4_status nvfp4_fp8_gemm_experts_dw(int64_t M, int64_t N, int64_t rows, int32
     if (rows < 0 || rows > MOST_ROWS) return NVFP4_ESHAPE;
     if (groups < 1 || groups > MAX_EXPERTS) return NVFP4_EINVAL;
     return product(FP8_EXPERTS_DW, M, N, FP8_BLOCK * fp8_slots(rows, groups), groups, offsets, rows, A_codes, A_scales, B_codes, B_scales, out, raw(out_dt), ldc,
-                   stream);
+                   nullptr, stream);
 }
 
 size_t nvfp4_moe_sort_workspace_bytes(int64_t pairs, int32_t groups)

@@ -59,8 +59,9 @@ __device__ __forceinline__ int group_of_slot(const int32_t *offsets, int groups,
 
 // out = A B^T of quantized operands [rows, 128 blocks].  FP8_DENSE: one product.  FP8_EXPERTS: the M rows of A and of the output are divided
 // by offsets among `groups` experts, expert e's against rows e N .. e N + N - 1 of B; rows of no expert become zeros.  FP8_EXPERTS_DW: one
-// M x N output for each expert, the contraction over its slots of A and B.
-enum Fp8Mode { FP8_DENSE, FP8_EXPERTS, FP8_EXPERTS_DW };
+// M x N output for each expert, the contraction over its slots of A and B.  FP8_DIVIDED: one product, the contraction divided among `groups` workgroups a tile, whose
+// sums meet in `partial`.
+enum Fp8Mode { FP8_DENSE, FP8_EXPERTS, FP8_EXPERTS_DW, FP8_DIVIDED };
 struct Fp8GemmArgs {
     int64_t M, N;
     int32_t blocks;                       // 128s of the operands' rows
@@ -70,6 +71,7 @@ struct Fp8GemmArgs {
     int64_t ldc;
     const int32_t *offsets;
     int32_t groups, total;                // total (FP8_EXPERTS_DW): the rows that the offsets divide
+    float *partial;                       // FP8_DIVIDED
     int32_t stream;                       // the output leaves by nontemporal stores (set by launch_fp8_gemm())
 };
 // The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
@@ -79,6 +81,9 @@ hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, 
 double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt);
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 int64_t compute_units();
+// Among how many workgroups that kernel divides a dense product's contraction (1: not at all), and the bytes that it then needs at `partial`
+int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, size_t *bytes, double *cost);
+size_t fp8_gemm_workspace(const Fp8GemmArgs &P, int out_dt);
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 
 // Routing

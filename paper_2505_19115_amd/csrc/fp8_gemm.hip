@@ -131,6 +131,31 @@ static hipError_t launch_tiles(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 // Per K tile: us of a round of these tiles, two workgroups a CU (128 x 40000 x 4096, 313 of these tiles or 209 of 256 x 192: 56.6 / 50.2 us, binary32 and 256 x 128 85 / 117)
 constexpr double K_TILE_BF16 = 0.95, K_TILE_F32 = 2.2;
 
+static double tiles_cost(int64_t tiles, int out_dt)
+{
+    const int64_t slots = 2 * compute_units();
+    return (double)((tiles + slots - 1) / slots) * (out_dt == NVFP4_F32 ? K_TILE_F32 : K_TILE_BF16);
+}
+// (expanding codes for binary32: 2000 x 2000 x 2000 44 / 34, 1056 x 2080 x 2784 36 / 43)
+static double thin_cost(const Fp8GemmArgs &P, int out_dt) { return fp8_gemm_thin_cost(P) * (out_dt == NVFP4_F32 ? 1.3 : 1.0); }
+
+// Parts of the contraction of a dense product (1: not divided), where that is quicker than every kernel that does not divide it (3 and 2.5 us: their start)
+static int parts_of(const Fp8GemmArgs &P, int out_dt, size_t *bytes)
+{
+    double cost;
+    const int parts = P.M > 0 && P.N > 0 && P.blocks > 0 ? fp8_gemm_parts(P, out_dt, bytes, &cost) : 1;
+    if (parts > 1 && cost < tiles_cost(f8g::tiles<FP8_DENSE>(P, 128, 128), out_dt) * P.blocks + 3.0 && cost < fp8_gemm_thin_cost(P) * P.blocks + 2.5) return parts;
+    *bytes = 0;
+    return 1;
+}
+
+size_t fp8_gemm_workspace(const Fp8GemmArgs &P, int out_dt)
+{
+    size_t bytes;
+    parts_of(P, out_dt, &bytes);
+    return bytes;
+}
+
 template <int MODE>
 static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
 {
@@ -138,14 +163,19 @@ static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
     // but 86 MB (4096 x 11008 x 4096) 154 -> 160, 128 MB the same.
     P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * (out_dt == NVFP4_F32 ? 4 : 2) >= ((int64_t)256 << 20);
     const int64_t mine = f8g::tiles<MODE>(P, 128, 128), slots = 2 * compute_units();
-    const double cost = (double)((mine + slots - 1) / slots) * (out_dt == NVFP4_F32 ? K_TILE_F32 : K_TILE_BF16);
+    const double cost = tiles_cost(mine, out_dt);
     const double wide = P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE, out_dt) : 1e30;
     // An expert's few rows: 8 on average for bf16, 16 for binary32 (us, few rows / tiles: 64 tokens, 8 of 64, 1024 x 2048 38 / 40 and 39 / 68; 128 tokens 51 / 41 and
     // 51 / 68; 64 tokens, 2 of 8, 4096 x 4096 51 / 30 and 52 / 74)
     if (MODE == FP8_EXPERTS && P.M <= (out_dt == NVFP4_BF16 ? 8 : 16) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     if (MODE == FP8_DENSE) {
-        // (expanding codes for binary32: 2000 x 2000 x 2000 44 / 34, 1056 x 2080 x 2784 36 / 43)
-        const double thin = fp8_gemm_thin_cost(P) * (out_dt == NVFP4_F32 ? 1.3 : 1.0);
+        size_t bytes;
+        const int parts = P.partial ? parts_of(P, out_dt, &bytes) : 1;
+        if (parts > 1) {
+            P.groups = parts;
+            return launch_fp8_gemm_wide(P, FP8_DIVIDED, out_dt, st);
+        }
+        const double thin = thin_cost(P, out_dt);
         if (thin < cost && thin < wide) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     }
     // A short contraction in few tiles: the larger ones take 1 to 2 us more to begin and end (experts 300 tokens, 3 of 10, 500 x 700 8.7 / 10.5, their weight

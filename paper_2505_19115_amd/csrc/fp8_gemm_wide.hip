@@ -119,7 +119,8 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     const int ntx = (int)((P.N + BN - 1) / BN);
     int *const group_row = reinterpret_cast<int *>(lds + G::GROUPS0), *const group_tile = group_row + MAX_EXPERTS + 2;
     int nty = (int)((P.M + BM - 1) / BM);
-    if (MODE != FP8_DENSE) {
+    constexpr bool DIVIDED = MODE == FP8_DIVIDED;
+    if (MODE == FP8_EXPERTS || MODE == FP8_EXPERTS_DW) {
         const int total = MODE == FP8_EXPERTS ? (int)P.M : P.total, groups = P.groups + (MODE == FP8_EXPERTS ? 1 : 0);
         if (wave == 0) {
             int row = 0, tiles = 0;
@@ -163,8 +164,8 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             e = id / (ntx * nty);
             tile_coords(id - e * ntx * nty, ntx, nty, ty, tx);
         } else {
-            tile_coords(id, ntx, MODE == FP8_EXPERTS_DW ? nty * P.groups : nty, ty, tx);
-            if (MODE == FP8_EXPERTS_DW) {
+            tile_coords(id, ntx, MODE == FP8_EXPERTS_DW || DIVIDED ? nty * P.groups : nty, ty, tx);
+            if (MODE == FP8_EXPERTS_DW || DIVIDED) {
                 e = ty / nty;
                 ty -= e * nty;
             }
@@ -189,6 +190,12 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                 T.count = rows > 0 ? (rows + KT - 1) / KT : 1;
                 keep = rows > 0 ? ~0u : 0u;
                 T.out = e * P.M;
+            }
+            if (DIVIDED) {
+                // (a part has a K tile at least)
+                T.k0 = (int)((int64_t)P.blocks * e / P.groups);
+                T.count = (int)((int64_t)P.blocks * (e + 1) / P.groups) - T.k0;
+                T.out = ((int64_t)e * nty + ty) * ntx + tx;
             }
             T.m0 = (int64_t)ty * BM;
             left = P.M - T.m0 < BM ? (int)(P.M - T.m0) : BM;
@@ -305,7 +312,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
     __builtin_amdgcn_s_barrier(); \
     asm volatile("" ::: "memory");
 
-    const int tiles = ntx * nty * (MODE == FP8_EXPERTS_DW ? P.groups : 1);
+    const int tiles = ntx * nty * (MODE == FP8_EXPERTS_DW || DIVIDED ? P.groups : 1);
     int id = (int)blockIdx.x;
     if (id >= tiles) return;
     uint32_t keep, next_keep = 0;
@@ -497,7 +504,25 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             }
             NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
         };
-        if (T.rows != BM || T.cols != BN) store(I0{}, I0{});
+        if constexpr (DIVIDED) {
+            // as they are, a fragment's 64 lanes together; fragments past the last row are nobody's
+            float4v_t *const to = reinterpret_cast<float4v_t *>(P.partial) + (T.out * 4 + wave) * (8 * FB * 64) + lane;
+#pragma unroll
+            for (int a = 0; a < 8; ++a) {
+                if (wm * 128 + 16 * a >= T.rows) continue;
+#pragma unroll
+                for (int b = 0; b < FB; ++b) {
+                    float4v_t v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (OUT_DT == NVFP4_F32) v[i] = acc[a][b][i];
+                        else asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][b][i]));
+                    }
+                    to[(a * FB + b) * 64] = v;
+                }
+            }
+            NVFP4_F8W_WAIT(ALL)
+        } else if (T.rows != BM || T.cols != BN) store(I0{}, I0{});
         else if (P.stream) store(I1{}, I1{});
         else store(I1{}, I0{});
         if (id >= tiles) break;
@@ -507,6 +532,52 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #undef NVFP4_F8W_BARRIER
 #undef NVFP4_F8W_WAIT
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the loads past the end, before the workgroup's LDS is another's)
+}
+
+// out = the sums of the parts in their order.  A lane has two fragments' places beside each other, eight columns of a row.
+template <int OUT_DT, int FB>
+__global__ __launch_bounds__(256) void fp8_gemm_join_kernel(Fp8GemmArgs P, int ntx, int nty)
+{
+    using namespace f8g;
+    constexpr int HB = FB / 2;
+    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+    // pair s of fragments, fragment row a, wave and tile of this wave of the grid
+    int id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int s = id % HB, a = id / HB % 8, wave = id / (8 * HB) % 4, tile = id / (32 * HB);
+    if (tile >= ntx * nty) return;
+    const int ty = tile / ntx, tx = tile - ty * ntx, wm = wave >> 1, wn = wave & 1;
+    const int64_t row = (int64_t)ty * f8w::BM + wm * 128 + 16 * a + c, col0 = (int64_t)tx * 32 * FB;
+    if (row - c >= P.M) return;
+    const float4v_t *from = reinterpret_cast<const float4v_t *>(P.partial) + ((int64_t)tile * 4 + wave) * (8 * FB * 64) + (a * FB + 2 * s) * 64 + lane;
+    const int64_t part = (int64_t)ntx * nty * (32 * FB * 64);
+    float4v_t v[2] = {from[0], from[64]};
+    for (int p = 1; p < P.groups; p += 4) {
+        float4v_t w[4][2];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float4v_t *const at = from + (p + u < P.groups ? p + u : p) * part;
+            w[u][0] = at[0];
+            w[u][1] = at[64];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p + u < P.groups) {
+                v[0] += w[u][0];
+                v[1] += w[u][1];
+            }
+    }
+    if (row >= P.M) return;
+    if constexpr (OUT_DT == NVFP4_F32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t col = col0 + f8w::column<OUT_DT, FB>(wn, 2 * s + h, 4 * q);
+            if (col < P.N) store_lane<OUT_DT, false>(P.out, row * P.ldc + col, __builtin_bit_cast(u32x4_t, v[h]), P.N - col < 16 ? (int)(P.N - col) : 16);
+        }
+    } else {
+        const float both[8] = {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+        const int64_t col = col0 + f8w::column<OUT_DT, FB>(wn, 2 * s, 4 * q);
+        if (col < P.N) store_lane<OUT_DT, false>(P.out, row * P.ldc + col, to_bf16(both), P.N - col < 16 ? (int)(P.N - col) : 16);
+    }
 }
 
 // Of the current device; a multiple of 8, so that a workgroup's tiles stay on its XCD's part of the walk
@@ -529,8 +600,12 @@ static hipError_t launch_wide(const Fp8GemmArgs &P, hipStream_t st)
     auto *k = fp8_gemm_wide_kernel<MODE, OUT_DT, FB>;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS_BYTES);
     if (once != hipSuccess) return once;
-    const int64_t tiles = f8g::tiles<MODE>(P, f8w::BM, G::BN), cus = compute_units();
+    const int64_t tiles = f8g::tiles<MODE == FP8_DIVIDED ? FP8_DENSE : MODE>(P, f8w::BM, G::BN) * (MODE == FP8_DIVIDED ? P.groups : 1), cus = compute_units();
     k<<<dim3((unsigned)(tiles < cus ? tiles : cus)), 256, G::LDS_BYTES, st>>>(P);
+    if (MODE == FP8_DIVIDED) {
+        const int ntx = (int)((P.N + G::BN - 1) / G::BN), nty = (int)((P.M + f8w::BM - 1) / f8w::BM);
+        fp8_gemm_join_kernel<OUT_DT, FB><<<dim3((unsigned)(ntx * nty * 4 * FB)), 256, 0, st>>>(P, ntx, nty);
+    }
     return hipGetLastError();
 }
 
@@ -564,17 +639,57 @@ double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt)
     return cost;
 }
 
+// A dense product with fewer tiles than CUs: the tiles' width and in how many parts of at least PART K tiles the contraction goes to a workgroup each.  The sums of the
+// parts leave as binary32 and are added by a second kernel: START, JOIN and JOIN_BYTES (a us, written and read) are what that costs, K tiles take longer than with all CUs
+// at work.  us, whole / divided: 512 x 4096 x 11008 71 / 36, 1000 x 4096 x 11008 75 / 53, 256 x 4096 x 11008 43 / 27, 128 x 4096 x 11008 35 / 24, 1000 x 1024 x 8192 32 / 21,
+// 512 x 4096 x 4096 24 / 21, binary32 1000 x 4096 x 4096 60 / 46; where this rule does not divide, 128 x 1024 x 8192 13.9 / 15.3, binary32 256 x 1024 x 8192 17.6 / 23.3.
+constexpr int PART = 4;
+constexpr double START = 3.0, JOIN = 5.0, JOIN_BYTES = 6e6;
+static int divided_width(const Fp8GemmArgs &P, int out_dt, int *parts, size_t *bytes, double *cost)
+{
+    const int64_t cus = compute_units(), rows = (P.M + 255) / 256;
+    const double k_tile[3] = {0.8, 1.0, 1.25};
+    int best = 4;
+    *parts = 1;
+    *bytes = 0;
+    *cost = 1e30;
+    for (int fb = 4; fb <= (out_dt == NVFP4_F32 ? 4 : 8); fb += 2) {
+        const int64_t tiles = rows * ((P.N + 32 * fb - 1) / (32 * fb));
+        for (int n = 1; n * tiles <= cus && (n == 1 || n * PART <= P.blocks); ++n) {
+            const double c = (P.blocks + n - 1) / n * (out_dt == NVFP4_F32 ? K_TILE_F32 : k_tile[fb / 2 - 2]) + START +
+                             (n == 1 ? 0.0 : JOIN + 2.0 * n * (tiles / rows * 32 * fb) * ((P.M + 15) / 16 * 16) * 4 / JOIN_BYTES);
+            if (c < *cost) {
+                *cost = c;
+                best = fb;
+                *parts = n;
+                *bytes = n == 1 ? 0 : (size_t)n * tiles * (256 * 32 * fb * 4);
+            }
+        }
+    }
+    return best;
+}
+
+int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, size_t *bytes, double *cost)
+{
+    int parts;
+    divided_width(P, out_dt, &parts, bytes, cost);
+    return parts;
+}
+
 template <int MODE>
 static hipError_t launch_width(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     if (out_dt == NVFP4_F32) return launch_wide<MODE, NVFP4_F32, 4>(P, st);
     double cost;
-    const int fb = width_of(P, MODE, out_dt, &cost);
+    int parts;
+    size_t bytes;
+    const int fb = MODE == FP8_DIVIDED ? divided_width(P, out_dt, &parts, &bytes, &cost) : width_of(P, MODE, out_dt, &cost);
     return fb == 4 ? launch_wide<MODE, NVFP4_BF16, 4>(P, st) : fb == 6 ? launch_wide<MODE, NVFP4_BF16, 6>(P, st) : launch_wide<MODE, NVFP4_BF16, 8>(P, st);
 }
 
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
 {
+    if (mode == FP8_DIVIDED) return launch_width<FP8_DIVIDED>(P, out_dt, st);
     return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, out_dt, st) : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, out_dt, st) : launch_width<FP8_EXPERTS_DW>(P, out_dt, st);
 }
 

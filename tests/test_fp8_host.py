@@ -159,3 +159,13 @@ def test_binding_refuses_host_tensors_and_wrong_types():
 def test_abi_types():
     # sizes come back whole, past 32 bits
     assert L.nvfp4_fp8_codes_bytes.restype is C.c_size_t and L.nvfp4_fp8_slots.restype is C.c_int64
+
+
+def test_divided_contraction_workspace():
+    # an output of few tiles and a long contraction wants scratch memory; a large one, a short contraction and no output do not
+    bytes_ = L.nvfp4_fp8_gemm_workspace_bytes
+    assert bytes_(512, 4096, 11008, 1) > 0 and bytes_(1000, 4096, 4096, 0) > 0
+    assert bytes_(512, 4096, 11008, 1) % (256 * 128 * 4) == 0
+    for M, N, K, dt in ((4096, 4096, 11008, 1), (512, 4096, 256, 1), (16, 4096, 4096, 1), (0, 4096, 11008, 1), (512, 0, 11008, 1), (512, 4096, 0, 1), (512, 4096, 11000, 1),
+                        (512, 4096, 11008, 5), (-1, 4096, 11008, 1), (1 << 40, 4096, 11008, 1)):
+        assert bytes_(M, N, K, dt) == 0

@@ -399,6 +399,33 @@ def test_few_rows_of_many_columns(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M, N, K", [(100, 4096, 11008), (257, 1000, 9001), (512, 3000, 6000), (777, 1025, 8192), (1000, 4096, 11008), (300, 129, 30000), (500, 200, 16257)])
+def test_divided_contraction(M, N, K, dtype):
+    # outputs of few tiles: with scratch memory their contraction is divided, without it is not; a pitched output, nothing beside it written
+    g = torch.Generator().manual_seed(M + N + K)
+    a, b = (nv.fp8_quantize(tensor(g, n, K).cuda())[0] for n in (M, N))
+    A, B = values_on_gpu(a), values_on_gpu(b)
+    ref = A @ B.t()
+    # (16 parts at most: as many more roundings)
+    most = A.abs() @ B.abs().t() * (lost(A.shape[1], dtype) + 16 * 2.0 ** -24) + (0 if dtype == torch.float32 else ROUNDED) * ref.abs() + 1e-300
+    whole = torch.empty(M, N, dtype=dtype, device="cuda")
+    P, tag = A.shape[1], 0 if dtype == torch.float32 else 1
+    stream = torch.cuda.current_stream().cuda_stream
+    assert nv.lib.nvfp4_fp8_gemm(M, N, P, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), whole.data_ptr(), tag, N, stream) == 0
+    wide = torch.full((M + 2, N + 5), 7.0, dtype=dtype, device="cuda")
+    out = nv.fp8_gemm(a, b, out=wide[1:-1, 3:3 + N])
+    for got in (whole, out):
+        assert bool(((got.double() - ref).abs() <= most).all())
+    assert bool((wide[0] == 7).all()) and bool((wide[-1] == 7).all()) and bool((wide[:, :3] == 7).all()) and bool((wide[:, 3 + N:] == 7).all())
+    assert torch.equal(out, nv.fp8_gemm(a, b, out_dtype=dtype))  # the same bits again
+    need = nv.lib.nvfp4_fp8_gemm_workspace_bytes(M, N, P, tag)
+    if need:  # too little of it is refused
+        less = torch.empty(need - 1, dtype=torch.uint8, device="cuda")
+        args = (M, N, P, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), whole.data_ptr(), tag, N)
+        assert nv.lib.nvfp4_fp8_gemm_ws(*args, less.data_ptr(), need - 1, stream) == nv.lib.nvfp4_fp8_gemm_ws(*args, None, need, stream) != 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_experts_large_tiles(dtype):
     # outputs of more tiles than CUs, uneven experts, weight gradients of many and of few tiles an expert
     g = torch.Generator().manual_seed(20)
