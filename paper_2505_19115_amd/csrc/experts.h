@@ -81,8 +81,9 @@ hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, 
 double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt);
 hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 int64_t compute_units();
-// Among how many workgroups that kernel divides a dense product's contraction (1: not at all), and the bytes that it then needs at `partial`
-int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, size_t *bytes, double *cost);
+// Among how many workgroups that kernel divides a dense product's contraction to be quickest (1: not at all, or not in less than `below` us), the bytes that it then
+// needs at `partial`, and its time in us
+int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, double below, size_t *bytes, double *cost);
 size_t fp8_gemm_workspace(const Fp8GemmArgs &P, int out_dt);
 hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
 

@@ -643,19 +643,19 @@ double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt)
 // parts leave as binary32 and are added by a second kernel: START, JOIN and JOIN_BYTES (a us, written and read) are what that costs, K tiles take longer than with all CUs
 // at work.  us, whole / divided: 512 x 4096 x 11008 71 / 36, 1000 x 4096 x 11008 75 / 53, 256 x 4096 x 11008 43 / 27, 128 x 4096 x 11008 35 / 24, 1000 x 1024 x 8192 32 / 21,
 // 512 x 4096 x 4096 24 / 21, binary32 1000 x 4096 x 4096 60 / 46; where this rule does not divide, 128 x 1024 x 8192 13.9 / 15.3, binary32 256 x 1024 x 8192 17.6 / 23.3.
-constexpr int PART = 4;
-constexpr double START = 3.0, JOIN = 5.0, JOIN_BYTES = 6e6;
+constexpr int PART = 4, MOST_PARTS = 16;
+constexpr double START = 3.0, JOIN = 5.0, JOIN_BYTES = 6e6, FEW_128 = 0.8, FEW_192 = 1.0, FEW_256 = 1.25;
 static int divided_width(const Fp8GemmArgs &P, int out_dt, int *parts, size_t *bytes, double *cost)
 {
     const int64_t cus = compute_units(), rows = (P.M + 255) / 256;
-    const double k_tile[3] = {0.8, 1.0, 1.25};
+    const double k_tile[3] = {FEW_128, FEW_192, FEW_256};
     int best = 4;
     *parts = 1;
     *bytes = 0;
     *cost = 1e30;
     for (int fb = 4; fb <= (out_dt == NVFP4_F32 ? 4 : 8); fb += 2) {
         const int64_t tiles = rows * ((P.N + 32 * fb - 1) / (32 * fb));
-        for (int n = 1; n * tiles <= cus && (n == 1 || n * PART <= P.blocks); ++n) {
+        for (int n = 1; n <= MOST_PARTS && n * tiles <= cus && (n == 1 || n * PART <= P.blocks); ++n) {
             const double c = (P.blocks + n - 1) / n * (out_dt == NVFP4_F32 ? K_TILE_F32 : k_tile[fb / 2 - 2]) + START +
                              (n == 1 ? 0.0 : JOIN + 2.0 * n * (tiles / rows * 32 * fb) * ((P.M + 15) / 16 * 16) * 4 / JOIN_BYTES);
             if (c < *cost) {
@@ -669,9 +669,10 @@ static int divided_width(const Fp8GemmArgs &P, int out_dt, int *parts, size_t *b
     return best;
 }
 
-int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, size_t *bytes, double *cost)
+int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, double below, size_t *bytes, double *cost)
 {
     int parts;
+    if (below < START + JOIN + PART * FEW_128) return 1;  // (small products: no search)
     divided_width(P, out_dt, &parts, bytes, cost);
     return parts;
 }
