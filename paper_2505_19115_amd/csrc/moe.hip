@@ -270,22 +270,31 @@ struct Piece {
     }
 };
 
+// Which row (of the launch's) a lane works on, G lanes side by side on one: the same in the wave where that is one row.
+template <int G>
+__device__ __forceinline__ int64_t row_of()
+{
+    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return G == 64 ? wave : wave * (64 / G) + (threadIdx.x & 63) / G;
+}
+
 // Walks a row in steps of U pieces a lane: body(at, n) with the byte offsets of a lane's pieces and how many elements each has there (0: none), and
 // whether all of them are whole, which is the same in the wave.
-template <int DT, int U, class F>
-__device__ __forceinline__ void walk(int64_t cols, int lane, F &&body)
+template <int DT, int U, int G, class F>
+__device__ __forceinline__ void walk(int64_t cols, F &&body)
 {
     constexpr int N = Piece<DT>::N;
-    for (int64_t c0 = 0; c0 < cols; c0 += 64 * N * U) {
+    const int lane = threadIdx.x & (G - 1);
+    for (int64_t c0 = 0; c0 < cols; c0 += G * N * U) {
         int64_t at[U];
         int n[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t c = c0 + (u * 64 + lane) * N;
+            const int64_t c = c0 + (u * G + lane) * N;
             at[u] = c * Piece<DT>::ESZ;
             n[u] = c + N <= cols ? N : c < cols ? (int)(cols - c) : 0;
         }
-        if (c0 + 64 * N * U <= cols) body(at, n, std::true_type{});
+        if (c0 + G * N * U <= cols) body(at, n, std::true_type{});
         else body(at, n, std::false_type{});
     }
 }
@@ -310,20 +319,19 @@ __device__ __forceinline__ void store(const Piece<DT> (&v)[U], uint8_t *row, con
 
 }  // namespace moe
 
-template <int DT, bool STREAMED>
+template <int DT, bool STREAMED, int G>
 __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k,
                                                          int64_t rows, uint8_t *out)
 {
     using namespace moe;
     constexpr int U = 2;
-    const int lane = threadIdx.x & 63;
-    const int64_t r = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r = row_of<G>();
     if (r >= rows) return;
     const int32_t pair = order[r];
     const int64_t src = pair < 0 || pair / top_k >= x_rows ? -1 : pair / top_k;
     const uint8_t *const from = x + src * ld * Piece<DT>::ESZ;
     uint8_t *const to = out + r * cols * Piece<DT>::ESZ;
-    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         Piece<DT> v[U];
         if (src >= 0) {
@@ -336,18 +344,17 @@ __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64
     });
 }
 
-// A wave for each token.  Two choices at a time: as many loads in flight.
-template <int DT, bool STREAMED>
+// G lanes for each token.  Two choices at a time: as many loads in flight.
+template <int DT, bool STREAMED, int G>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position,
                                                           int64_t tokens, int32_t top_k, uint8_t *out)
 {
     using namespace moe;
     constexpr int U = 2, N = Piece<DT>::N;
-    const int lane = threadIdx.x & 63;
-    const int64_t t = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = cols * Piece<DT>::ESZ;
+    const int64_t t = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (t >= tokens) return;
     const int32_t *const places = position + t * top_k;
-    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         float sum[U][N];
 #pragma unroll
@@ -376,20 +383,20 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int6
     });
 }
 
-// A wave for each pair; behind them the waves that clear the rows of dy past the last kept pair
-template <int DT, bool STREAMED>
+// G lanes for each pair; behind them those that clear the rows of dy past the last kept pair
+template <int DT, bool STREAMED, int G>
 __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dout, const uint8_t *y, int64_t rows, int64_t cols, const float *weights,
                                                               const int32_t *position, const int32_t *kept, int64_t pairs, int32_t top_k, uint8_t *dy,
                                                               float *dweights)
 {
     using namespace moe;
     constexpr int U = 2, N = Piece<DT>::N;
-    const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = cols * Piece<DT>::ESZ;
+    const int lane = threadIdx.x & (G - 1);
+    const int64_t id = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (id >= pairs) {
-        const int64_t clearing = (int64_t)gridDim.x * 4 - pairs;
+        const int64_t clearing = (int64_t)gridDim.x * (256 / G) - pairs;
         for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
-            walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+            walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
                 Piece<DT> v[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
@@ -406,7 +413,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
     uint8_t *const to = dy + p * row;
     const float w = weights[id];
     float dot = 0.0f;
-    walk<DT, U>(cols, lane, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         Piece<DT> a[U], b[U];
         load<DT, W, false>(a, up, at, n);
@@ -424,7 +431,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
         store<DT, W>(a, to, at, n);
     });
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+    for (int d = G / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
     if (lane == 0) dweights[id] = dot;
 }
 
@@ -438,13 +445,32 @@ static bool streams(const void *rows, int64_t n, int64_t cols, int dt)
     return row % 128 == 0 && reinterpret_cast<uintptr_t>(rows) % 128 == 0 && n * row >= ((int64_t)STREAM_MB << 20);
 }
 
+// Lanes of a row: a row of at most 2 G pieces leaves the others of a wave without work
+static int lanes_of(int64_t cols, int dt)
+{
+    const int64_t pieces = (cols * (dt == NVFP4_BF16 ? 2 : 4) + 15) / 16;
+    return pieces <= 16 ? 8 : pieces <= 32 ? 16 : pieces <= 64 ? 32 : 64;
+}
+// (rows of a wave's groups of lanes)
+static dim3 grid_of(int64_t rows, int lanes) { return dim3((unsigned)((rows + 256 / lanes - 1) / (256 / lanes))); }
+
+#define NVFP4_MOE_PICK(kernel, dt, s, lanes)                                                            \
+    ((dt) == NVFP4_BF16 ? ((lanes) == 8 ? kernel<NVFP4_BF16, false, 8>                                  \
+                           : (lanes) == 16 ? kernel<NVFP4_BF16, false, 16>                              \
+                           : (lanes) == 32 ? kernel<NVFP4_BF16, false, 32>                              \
+                           : (s) ? kernel<NVFP4_BF16, true, 64> : kernel<NVFP4_BF16, false, 64>)        \
+                        : ((lanes) == 8 ? kernel<NVFP4_F32, false, 8>                                   \
+                           : (lanes) == 16 ? kernel<NVFP4_F32, false, 16>                               \
+                           : (lanes) == 32 ? kernel<NVFP4_F32, false, 32>                               \
+                           : (s) ? kernel<NVFP4_F32, true, 64> : kernel<NVFP4_F32, false, 64>))
+
 hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out,
                              hipStream_t st)
 {
     const bool s = top_k == 1 && ld == cols && streams(x, x_rows, cols, dt);
-    auto *k = dt == NVFP4_BF16 ? (s ? moe_gather_kernel<NVFP4_BF16, true> : moe_gather_kernel<NVFP4_BF16, false>)
-                               : (s ? moe_gather_kernel<NVFP4_F32, true> : moe_gather_kernel<NVFP4_F32, false>);
-    k<<<dim3((unsigned)((rows + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
+    const int lanes = lanes_of(cols, dt);
+    auto *k = NVFP4_MOE_PICK(moe_gather_kernel, dt, s, lanes);
+    k<<<grid_of(rows, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
                                                        reinterpret_cast<uint8_t *>(out));
     return hipGetLastError();
 }
@@ -453,9 +479,9 @@ hipError_t launch_moe_combine(const void *y, int dt, int64_t y_rows, int64_t col
                               int32_t top_k, void *out, hipStream_t st)
 {
     const bool s = streams(y, y_rows, cols, dt);
-    auto *k = dt == NVFP4_BF16 ? (s ? moe_combine_kernel<NVFP4_BF16, true> : moe_combine_kernel<NVFP4_BF16, false>)
-                               : (s ? moe_combine_kernel<NVFP4_F32, true> : moe_combine_kernel<NVFP4_F32, false>);
-    k<<<dim3((unsigned)((tokens + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position, tokens, top_k,
+    const int lanes = lanes_of(cols, dt);
+    auto *k = NVFP4_MOE_PICK(moe_combine_kernel, dt, s, lanes);
+    k<<<grid_of(tokens, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position, tokens, top_k,
                                                          reinterpret_cast<uint8_t *>(out));
     return hipGetLastError();
 }
@@ -465,11 +491,13 @@ hipError_t launch_moe_combine_bwd(const void *dout, const void *y, int dt, int64
 {
     const int64_t pairs = tokens * top_k, clearing = rows < 256 ? rows : 256;
     const bool s = streams(y, rows, cols, dt);
-    auto *k = dt == NVFP4_BF16 ? (s ? moe_combine_bwd_kernel<NVFP4_BF16, true> : moe_combine_bwd_kernel<NVFP4_BF16, false>)
-                               : (s ? moe_combine_bwd_kernel<NVFP4_F32, true> : moe_combine_bwd_kernel<NVFP4_F32, false>);
-    k<<<dim3((unsigned)((pairs + clearing + 3) / 4)), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols,
+    const int lanes = lanes_of(cols, dt);
+    auto *k = NVFP4_MOE_PICK(moe_combine_bwd_kernel, dt, s, lanes);
+    k<<<grid_of(pairs + clearing, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols,
                                                                    weights, position, kept, pairs, top_k, reinterpret_cast<uint8_t *>(dy), dweights);
     return hipGetLastError();
 }
+
+#undef NVFP4_MOE_PICK
 
 }  // namespace nvfp4
