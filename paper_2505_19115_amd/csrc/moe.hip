@@ -278,8 +278,8 @@ __device__ __forceinline__ int64_t row_of()
     return G == 64 ? wave : wave * (64 / G) + (threadIdx.x & 63) / G;
 }
 
-// Walks a row in steps of U pieces a lane: body(at, n) with the byte offsets of a lane's pieces and how many elements each has there (0: none), and
-// whether all of them are whole, which is the same in the wave.
+// Walks a row in steps of U pieces a lane: body(at, n, again, whole) with the byte offsets of a lane's pieces, how many elements each has there (0: none), how many of
+// them the piece before has too (a row's last piece ends with the row), and whether all pieces are there and none overlaps, which is the same in the wave.
 template <int DT, int U, int G, class F>
 __device__ __forceinline__ void walk(int64_t cols, F &&body)
 {
@@ -287,15 +287,17 @@ __device__ __forceinline__ void walk(int64_t cols, F &&body)
     const int lane = threadIdx.x & (G - 1);
     for (int64_t c0 = 0; c0 < cols; c0 += G * N * U) {
         int64_t at[U];
-        int n[U];
+        int n[U], again[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t c = c0 + (u * G + lane) * N;
-            at[u] = c * Piece<DT>::ESZ;
-            n[u] = c + N <= cols ? N : c < cols ? (int)(cols - c) : 0;
+            const int left = cols - c < N ? (int)(cols - c) : N;
+            again[u] = left > 0 && cols >= N ? N - left : 0;
+            at[u] = (c - again[u]) * Piece<DT>::ESZ;
+            n[u] = left > 0 ? left + again[u] : 0;
         }
-        if (c0 + G * N * U <= cols) body(at, n, std::true_type{});
-        else body(at, n, std::false_type{});
+        if (c0 + G * N * U <= cols) body(at, n, again, std::true_type{});
+        else body(at, n, again, std::false_type{});
     }
 }
 template <int DT, bool WHOLE, bool STREAMED, int U>
@@ -304,7 +306,8 @@ __device__ __forceinline__ void load(Piece<DT> (&v)[U], const uint8_t *row, cons
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (WHOLE || n[u] == Piece<DT>::N) v[u].template load<STREAMED>(row + at[u]);
-        else v[u].load_some(row + at[u], n[u]);
+        else if (n[u] > 0) v[u].load_some(row + at[u], n[u]);
+        else v[u].w = u32x4_t{0, 0, 0, 0};
     }
 }
 template <int DT, bool WHOLE, int U>
@@ -313,7 +316,7 @@ __device__ __forceinline__ void store(const Piece<DT> (&v)[U], uint8_t *row, con
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (WHOLE || n[u] == Piece<DT>::N) v[u].store(row + at[u]);
-        else v[u].store_some(row + at[u], n[u]);
+        else if (n[u] > 0) v[u].store_some(row + at[u], n[u]);
     }
 }
 
@@ -331,7 +334,7 @@ __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64
     const int64_t src = pair < 0 || pair / top_k >= x_rows ? -1 : pair / top_k;
     const uint8_t *const from = x + src * ld * Piece<DT>::ESZ;
     uint8_t *const to = out + r * cols * Piece<DT>::ESZ;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         Piece<DT> v[U];
         if (src >= 0) {
@@ -354,7 +357,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int6
     const int64_t t = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (t >= tokens) return;
     const int32_t *const places = position + t * top_k;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         float sum[U][N];
 #pragma unroll
@@ -396,7 +399,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
     if (id >= pairs) {
         const int64_t clearing = (int64_t)gridDim.x * (256 / G) - pairs;
         for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
-            walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+            walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
                 Piece<DT> v[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
@@ -413,7 +416,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
     uint8_t *const to = dy + p * row;
     const float w = weights[id];
     float dot = 0.0f;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], auto whole) {
+    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         Piece<DT> a[U], b[U];
         load<DT, W, false>(a, up, at, n);
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = w * a[u].get(i);
-                dot = __builtin_fmaf(a[u].get(i), b[u].get(i), dot);
+                if (W || i >= again[u]) dot = __builtin_fmaf(a[u].get(i), b[u].get(i), dot);
             }
             a[u].set(v);
         }
