@@ -188,3 +188,24 @@ def test_refusals():
         nv.moe_gather(x, o.order, 0)
     assert nv.moe_combine(y[:, :0].contiguous(), o.position, w).shape == (10, 0)
     assert nv.moe_gather(x, o.order[:0], 2).shape == (0, 16)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [2, 3, 4, 5, 7, 8, 9, 15, 63, 64, 65, 127, 128, 129, 131, 255, 256, 257, 263, 511, 512, 513, 519, 1023, 1025])
+def test_widths(D, dtype):
+    # rows by 8, 16, 32 and 64 lanes, with and without a last piece that overlaps the one before; a lane adds at most 16 products of a row at a time, 64 lanes 6 sums
+    T, k, E = 37, 3, 4
+    o, x, y, w = case(8, T, k, E, D, dtype)
+    order, pos, kept = o.order.cpu().long(), o.position.cpu().long(), int(o.offsets[-1])
+    ref = torch.where((order >= 0)[:, None], x[order.clamp(min=0) // k], torch.zeros((), dtype=dtype))
+    assert torch.equal(nv.moe_gather(x.cuda(), o.order, k).cpu(), ref)
+    rows = torch.where((pos >= 0)[..., None], y.double()[pos.clamp(min=0)], torch.zeros((), dtype=torch.float64))
+    got, ref = nv.moe_combine(y.cuda(), o.position, w.cuda()).cpu().double(), (rows * w.double()[..., None]).sum(1)
+    assert bool(((got - ref).abs() <= k * 2.0 ** -24 * (rows * w.double()[..., None]).abs().sum(1) + OWN[dtype] * ref.abs() * (1 + 2.0 ** -6) + 1e-300).all())
+    dy, dw = (t.cpu() for t in nv.moe_combine_bwd(x.cuda(), y.cuda(), w.cuda(), o.position, o.offsets))
+    ref = torch.zeros(T * k, D, dtype=torch.float64)
+    t = torch.arange(T).repeat_interleave(k).view(T, k)[pos >= 0]
+    ref[pos[pos >= 0]] = x.double()[t] * w.double()[pos >= 0][:, None]
+    assert bool(((dy.double() - ref).abs() <= (OWN[dtype] * (1 + 2.0 ** -6) + 2.0 ** -24) * ref.abs()).all()) and bool((dy[kept:] == 0).all())
+    products = x.double()[:, None] * rows
+    assert bool(((dw.double() - products.sum(-1)).abs() <= (D / 64 + 22) * 2.0 ** -24 * products.abs().sum(-1) + 1e-300).all())
