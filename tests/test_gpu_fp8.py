@@ -523,6 +523,33 @@ def test_graph():
         assert all(torch.equal(a, b) for a, b in zip(ref, got)), seed
 
 
+def test_graph_of_a_divided_contraction():
+    # a product that brings its own scratch memory, on two streams and captured, replayed between eager calls with memory of their own
+    g = torch.Generator().manual_seed(40)
+    held = [tensor(g, 512, 8000).cuda(), tensor(g, 1000, 8000).cuda()]
+    assert nv.lib.nvfp4_fp8_gemm_workspace_bytes(512, 1000, 8064, 1) > 0
+    step = lambda x, w: nv.fp8_gemm(nv.fp8_quantize(x)[0], nv.fp8_quantize(w)[0])  # noqa: E731
+    ref, side = step(*held), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(ref, got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*held)
+    for _ in range(4):
+        new = [tensor(g, 512, 8000).cuda(), tensor(g, 1000, 8000).cuda()]
+        for h, n in zip(held, new):
+            h.copy_(n)
+        graph.replay()
+        others = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(8)]  # (what eager work allocates between)
+        ref = step(*new)
+        torch.cuda.synchronize()
+        assert torch.equal(ref, got) and len(others) == 8
+
+
 def test_example():
     import importlib.util
     import os
