@@ -132,15 +132,25 @@ __device__ __forceinline__ uint32_t four_scales(const uint8_t *scales, int64_t r
 //     off at 2^-13 of the power of two under its group's largest (the other 8-bit forms lose as much), and adds the groups in binary32: what is lost is at
 //     most 7 2^-13 = 8.5e-4 of sum |a||b|, reached only where single products stand far above the seven beside them, and 1.5e-5 of the result's norm for
 //     normal data, where rounding to bf16 takes 1.7e-3 of the norm.
-//   binary32 outputs: the codes become bf16, scale included (v_cvt_scalef32_pk_bf16_fp8: both exact), for v_mfma_f32_16x16x32_bf16, whose sums
-//     are binary32 (1e-7 of the norm), at half the rate and for 32 conversions a lane.
+//   binary32 outputs: the codes become bf16, scale included (v_cvt_scalef32_pk_bf16_fp8), for v_mfma_f32_16x16x32_bf16, whose sums
+//     are binary32 (1e-7 of the norm), at half the rate and for 32 conversions a lane.  That is exact for scale bytes LEAST .. MOST: below, the smallest codes
+//     need bits under bf16's least subnormal 2^-133, above, 448 * 2^(byte - 127) passes its largest number (a finite tensor's byte is 247 from
+//     1.75 * 2^127 on, torch.finfo(torch.bfloat16).min among them).  A wave that meets a block beyond these sums its outputs by multiply_codes().
+constexpr uint32_t LEAST = 3, MOST = 246;
 struct Codes {
     u32x4_t lo, hi;  // chunks q and q + 4 of a row's eight
+    __device__ __forceinline__ bool any() const
+    {
+        return ((lo[0] | lo[1] | lo[2] | lo[3] | hi[0] | hi[1] | hi[2] | hi[3]) & 0x7F7F7F7Fu) != 0;
+    }
+    // whether bf16 may not hold these codes with this scale (a block of zeros has byte 0, which costs nothing)
+    __device__ __forceinline__ bool beyond(uint32_t byte) const { return byte > MOST || (byte < LEAST && any()); }
     __device__ __forceinline__ int8v_t all() const
     {
         return int8v_t{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
     }
 };
+__device__ __forceinline__ Codes codes_at(const uint8_t *p) { return {*reinterpret_cast<const u32x4_t *>(p), *reinterpret_cast<const u32x4_t *>(p + 64)}; }
 struct Expanded {
     bf16x8_t v[4];
 };
@@ -162,10 +172,50 @@ __device__ __forceinline__ Expanded expand(const Codes &x, uint32_t byte)
         }
     return r;
 }
+// Whether one of four bytes is below LEAST or above MOST
+__device__ __forceinline__ bool odd_bytes(uint32_t v)
+{
+    const uint32_t low = v & 0x7F7F7F7Fu, top = 0x80808080u, from_least = low + (0x80 - LEAST) * 0x01010101u, past_most = low + (0xFF - MOST) * 0x01010101u;
+    return ((~(v | from_least) | (v & past_most)) & top) != 0;
+}
 // step i of four
 __device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, const Expanded &a, int i)
 {
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], acc, 0, 0, 0);
+}
+
+// Whether one of K tiles kt, kt + step, ... below `end` is a block that bf16 does not hold
+__device__ __forceinline__ bool any_beyond(const uint8_t *codes, const uint8_t *scale, int64_t rows, int kt, int step, int end)
+{
+    bool beyond = false;
+#pragma unroll 4
+    for (; kt < end; kt += step) {
+        const Codes x = codes_at(codes + (int64_t)kt * KT);
+        const uint32_t byte = scale[kt * rows];
+        beyond |= (byte > MOST) | ((byte < LEAST) & x.any());
+    }
+    return beyond;
+}
+// The sum of K tiles kt, kt + step, ... below `end` of one fragment of each operand, whatever the scales: a tile's codes are multiplied, whose products and sums
+// binary32 holds as it holds any, and the sum takes both scales.  a, b: the lane's first chunk of its row at K tile 0; sa, sb: its row's first scale byte.
+// Byte 255 is no number.  Slow, straight from memory: what a wave does again where bf16 did not hold one of its blocks.
+__device__ __forceinline__ float4v_t multiply_codes(const Fp8GemmArgs &P, const uint8_t *b, const uint8_t *sb, const uint8_t *a, const uint8_t *sa, int kt, int step, int end)
+{
+    float4v_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (; kt < end; kt += step) {
+        const Expanded eb = expand(codes_at(b + (int64_t)kt * KT), 127), ea = expand(codes_at(a + (int64_t)kt * KT), 127);
+        const uint32_t mine = sb[kt * P.b_rows], s = sa[kt * P.a_rows];
+        float4v_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) multiply(sum, eb, ea, i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = (uint32_t)__shfl((int)mine, 4 * (int)((threadIdx.x & 63) >> 4) + i);  // acc's rows of B: positions 4 q .. 4 q + 3
+            acc[i] += r == 255 || s == 255 ? __uint_as_float(0x7FC00000u) : __builtin_ldexpf(sum[i], (int)(r + s) - 254);
+        }
+    }
+    return acc;
 }
 
 // n of four columns of one row

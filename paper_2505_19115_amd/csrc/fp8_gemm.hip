@@ -64,6 +64,10 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
 #pragma unroll
         for (int b = 0; b < 4; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
     const int ma = wm * 64 < T.rows ? wm * 64 : 0, nb = wn * 64 < T.cols ? wn * 64 : 0;  // (a wave past the edge computes what nobody stores)
+    // bytes of rows 4 c .. 4 c + 3 that are the tile's (four_scales())
+    auto bytes_of = [&](int rows) -> uint32_t { return rows >= 4 ? ~0u : rows > 0 ? (1u << (8 * rows)) - 1 : 0u; };
+    const uint32_t rows_a = bytes_of(T.rows - ma - 4 * c), rows_b = bytes_of(T.cols - nb - 4 * c);
+    bool beyond = false;
     if (T.count > 0) {
         fetch(0);
         stash(0);
@@ -80,6 +84,14 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
             return {*reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s0), *reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s1)};
         };
         if constexpr (OUT_DT == NVFP4_F32) {
+            // (blocks of the rows that there are)
+            if (__builtin_expect(__ballot(odd_bytes((sa & rows_a) | (~rows_a & 0x7F7F7F7Fu)) || odd_bytes((sb & rows_b) | (~rows_b & 0x7F7F7F7Fu))) != 0, 0)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    beyond |= ((rows_a >> (8 * j)) & 255) != 0 && read(A, j).beyond((sa >> (8 * j)) & 255);
+                    beyond |= ((rows_b >> (8 * j)) & 255) != 0 && read(B, j).beyond((sb >> (8 * j)) & 255);
+                }
+            }
             Expanded fa[4];
 #pragma unroll
             for (int a = 0; a < 4; ++a) fa[a] = expand(read(A, a), (sa >> (8 * a)) & 255);
@@ -106,6 +118,21 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
         }
         if (more) stash((kt + 1) & 1);
         __syncthreads();
+    }
+    if (OUT_DT == NVFP4_F32 && __builtin_expect(__ballot(beyond) != 0, 0)) {
+#pragma unroll 1
+        for (int f = 0; f < 16; ++f) {
+            const int r = ma + 4 * c + (f >> 2), s = nb + 4 * c + (f & 3);
+            const int64_t ra = T.m0 + (r < T.rows ? r : T.rows - 1), rb = T.b0 + T.n0 + (s < T.cols ? s : T.cols - 1);
+            const float4v_t v = multiply_codes(P, P.B + rb * pitch + q * 16, P.B_scales + rb, P.A + ra * pitch + q * 16, P.A_scales + ra, T.k0, 1, T.k0 + T.count);
+            const int row = wm * 64 + 4 * c + (f >> 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int col = wn * 64 + 16 * q + 4 * i + (f & 3);
+                if (row < T.rows && col < T.cols) reinterpret_cast<float *>(P.out)[(T.out + T.m0 + row) * P.ldc + T.n0 + col] = v[i];
+            }
+        }
+        return;
     }
 #pragma unroll
     for (int a = 0; a < 4; ++a) {

@@ -327,6 +327,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
             for (int b = 0; b < FB; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
         Codes A[8], B[FB];
+        bool beyond = false;  // (binary32 outputs) a block that bf16 does not hold
         auto read_a = [&](int st, int f, int h) { (h ? A[f].hi : A[f].lo) = *reinterpret_cast<const u32x4_t *>(baseA[st][h] + 16 * f * KT); };
         auto read_b = [&](int st, int f, int h) { (h ? B[f].hi : B[f].lo) = *reinterpret_cast<const u32x4_t *>(baseB[st][h] + 16 * f * KT); };
         // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
@@ -362,6 +363,24 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
                             for (int a = 0; a < 4; ++a) multiply(acc[4 * ha + a][f], EB[f], EA[a], i);
                 };
+                // Blocks that bf16 does not hold, in a tile with scale bytes that may be such.  (A0 and P are in registers, and their places others' to write; Q and A1
+                // stay until the barrier.)
+                uint32_t least = ~0u, most = 0;
+#pragma unroll
+                for (int f = 0; f < 8 + FB; ++f) {
+                    const uint32_t byte = f < 8 ? SA[ST][f >> 2][f & 3] : SB[ST][(f - 8) >> 2][f & 3];
+                    least = byte < least ? byte : least;
+                    most = byte > most ? byte : most;
+                }
+                if (__builtin_expect(__ballot(least < LEAST || most > MOST) != 0, 0)) {
+                    auto there = [&](const uint8_t *const (&base)[2], int f) -> Codes {
+                        return {*reinterpret_cast<const u32x4_t *>(base[0] + 16 * f * KT), *reinterpret_cast<const u32x4_t *>(base[1] + 16 * f * KT)};
+                    };
+#pragma unroll
+                    for (int f = 0; f < 8; ++f) beyond |= (f < 4 ? A[f] : there(baseA[ST], f)).beyond(SA[ST][f >> 2][f & 3]);
+#pragma unroll
+                    for (int f = 0; f < FB; ++f) beyond |= (f / HB == ST ? B[f] : there(baseB[ST], f)).beyond(SB[ST][f >> 2][f & 3]);
+                }
                 f8w::each<0, G::FIRST>([&](auto i) { request_first(stage, i); });
                 expand_a(0);
                 expand_b(ST);
@@ -504,7 +523,20 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             }
             NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
         };
-        if constexpr (DIVIDED) {
+        bool again = false;
+        if constexpr (OUT_DT == NVFP4_F32) again = keep != 0 && __ballot(beyond) != 0;  // (what no row holds may be anything)
+        if (__builtin_expect(again, 0)) {
+#pragma unroll 1
+            for (int f = 0; f < 8 * FB; ++f) {
+                const int row = wm * 128 + 16 * (f / FB) + c, s = f8w::column<OUT_DT, FB>(wn, f % FB, c), col = f8w::column<OUT_DT, FB>(wn, f % FB, 4 * q);
+                const int64_t ra = T.m0 + (row < T.rows ? row : T.rows - 1), rb = T.b0 + T.n0 + (s < T.cols ? s : T.cols - 1);
+                const float4v_t v = multiply_codes(P, P.B + rb * pitch + q * 16, P.B_scales + rb, P.A + ra * pitch + q * 16, P.A_scales + ra, T.k0, 1, T.k0 + T.count);
+                if (DIVIDED) reinterpret_cast<float4v_t *>(P.partial)[(T.out * 4 + wave) * (8 * FB * 64) + f * 64 + lane] = v;
+                else if (row < T.rows && col < T.cols)
+                    store_lane<OUT_DT, false>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col, __builtin_bit_cast(u32x4_t, v) & keep, T.cols - col);
+            }
+            NVFP4_F8W_WAIT(ALL)
+        } else if constexpr (DIVIDED) {
             // as they are, a fragment's 64 lanes together; fragments past the last row are nobody's
             float4v_t *const to = reinterpret_cast<float4v_t *>(P.partial) + (T.out * 4 + wave) * (8 * FB * 64) + lane;
 #pragma unroll
