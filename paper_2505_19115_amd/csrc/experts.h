@@ -10,6 +10,11 @@ namespace nvfp4 {
 constexpr int FP8_BLOCK = 128;      // elements that share a scale, contraction elements of a K tile, bytes of a row of one
 constexpr int MAX_EXPERTS = 512;
 
+// A launch counts the threads along an axis in 32 bits: workgroups 0 .. n - 1 in rows of LAUNCH_ROW, the last of which may have some past n.
+constexpr int64_t LAUNCH_ROW = (int64_t)1 << 22;  // (512 threads each at the most)
+inline dim3 launch_grid(int64_t n) { return n <= LAUNCH_ROW ? dim3((unsigned)n) : dim3((unsigned)LAUNCH_ROW, (unsigned)((n + LAUNCH_ROW - 1) / LAUNCH_ROW)); }
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // A tensor to quantize in blocks of 128: rows, columns or both.  With `order` its row r is row order[r] / top_k of x (none: zeros).
 // With `offsets` [groups + 1] the column blocks start anew at each group's first row.
 struct Fp8QuantArgs {

@@ -25,11 +25,12 @@ struct Tile {
 
 // Tiles of a launch; of the experts' product the most there can be: every group of rows (the rows of no expert are one) may have one that is not full.
 template <int MODE>
-inline int64_t tiles(const Fp8GemmArgs &P, int BM, int BN)
+__host__ __device__ inline int64_t tile_rows(const Fp8GemmArgs &P, int BM)
 {
-    const int64_t ntx = (P.N + BN - 1) / BN, nty = (P.M + BM - 1) / BM;
-    return ntx * (MODE == FP8_EXPERTS ? P.M / BM + (P.M < P.groups + 1 ? P.M : P.groups + 1) : MODE == FP8_EXPERTS_DW ? nty * P.groups : nty);
+    return MODE == FP8_EXPERTS ? P.M / BM + (P.M < P.groups + 1 ? P.M : P.groups + 1) : (P.M + BM - 1) / BM * (MODE == FP8_EXPERTS_DW ? P.groups : 1);
 }
+template <int MODE>
+inline int64_t tiles(const Fp8GemmArgs &P, int BM, int BN) { return (P.N + BN - 1) / BN * tile_rows<MODE>(P, BM); }
 
 // Tile `n` of those that the groups of rows have one after the other, step rows each: its group (`groups` for the rows of no expert, -1: there are not so many), first
 // row and the rows from there on to the group's end.  Every wave asks for itself.  (With a place for each tile that a group might have, found from
@@ -72,13 +73,17 @@ template <int MODE>
 __device__ __forceinline__ Tile find_tile(const Fp8GemmArgs &P, unsigned id, int BM, int BN)
 {
     Tile T;
-    const int ntx = (int)((P.N + BN - 1) / BN);
+    const int ntx = (int)((P.N + BN - 1) / BN), nty = (int)tile_rows<MODE>(P, BM);
     T.k0 = 0;
     T.count = P.blocks;
     T.b0 = 0;
     T.out = 0;
+    if (id >= (unsigned)ntx * (unsigned)nty) {
+        T.rows = 0;
+        return T;
+    }
     int ty, tx;
-    tile_coords((int)id, ntx, (int)(gridDim.x / (unsigned)ntx), ty, tx);
+    tile_coords((int)id, ntx, nty, ty, tx);
     int64_t left;
     if (MODE == FP8_EXPERTS) {
         // rows past the last expert's are a group of their own, with no K tile: zeros

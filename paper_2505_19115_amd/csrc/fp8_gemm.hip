@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 15, q = lane >> 4;
     const int wm = wave >> 1, wn = wave & 1;
-    const Tile T = find_tile<MODE>(P, blockIdx.x, BM, BN);
+    const Tile T = find_tile<MODE>(P, workgroup(), BM, BN);
     if (T.rows <= 0) return;
     const int64_t pitch = (int64_t)P.blocks * KT;
 
@@ -151,7 +151,7 @@ static hipError_t launch_tiles(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     constexpr int BM = 128, BN = 128, LDS = 2 * (BM + BN) * FP8_BLOCK;
     auto *k = out_dt == NVFP4_F32 ? fp8_gemm_kernel<MODE, NVFP4_F32> : fp8_gemm_kernel<MODE, NVFP4_BF16>;
-    k<<<dim3((unsigned)f8g::tiles<MODE>(P, BM, BN)), 256, LDS, st>>>(P);
+    k<<<launch_grid(f8g::tiles<MODE>(P, BM, BN)), 256, LDS, st>>>(P);
     return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
     using namespace f8g;
     __shared__ float4v_t sums[NW][MT * TN][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
-    const Tile T = find_tile<MODE>(P, blockIdx.x, 16 * MT, 16 * TN);
+    const Tile T = find_tile<MODE>(P, workgroup(), 16 * MT, 16 * TN);
     if (T.rows <= 0) return;
     const int64_t pitch = (int64_t)P.blocks * KT;
     // (rows past the edge repeat the last one)
@@ -136,7 +136,7 @@ template <int MODE, int MT, int TN, int U, int NW>
 static hipError_t launch_batches(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     auto *k = out_dt == NVFP4_F32 ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, TN, U, NW> : fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, TN, U, NW>;
-    k<<<dim3((unsigned)f8g::tiles<MODE>(P, 16 * MT, 16 * TN)), 64 * NW, 0, st>>>(P);
+    k<<<launch_grid(f8g::tiles<MODE>(P, 16 * MT, 16 * TN)), 64 * NW, 0, st>>>(P);
     return hipGetLastError();
 }
 

@@ -178,8 +178,8 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(Fp8QuantArgs P, 
 {
     using namespace f8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane & 15;
-    const unsigned up = blockIdx.x / across;
-    const int kb = __builtin_amdgcn_readfirstlane((int)(blockIdx.x - up * across) * 4 + wave);
+    const unsigned id = workgroup(), up = id / across;
+    const int kb = __builtin_amdgcn_readfirstlane((int)(id - up * across) * 4 + wave);
     if (kb >= blocks) return;
     const int64_t r0 = ((int64_t)up * 4 + (lane >> 4)) * RPG;
     const int64_t col = (int64_t)kb * FP8_BLOCK + in * 8;
@@ -206,8 +206,9 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
     __shared__ __attribute__((aligned(16))) uint8_t turned[FP8_BLOCK * PITCH];
     __shared__ uint32_t top[4][FP8_BLOCK];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, cg = tid & 15, rg = tid >> 4;
-    const int tile = (int)(blockIdx.x % (unsigned)col_tiles);
-    const int at = (int)(blockIdx.x / (unsigned)col_tiles);
+    const unsigned id = workgroup();
+    const int tile = (int)(id % (unsigned)col_tiles);
+    const int at = (int)(id / (unsigned)col_tiles);
     int64_t row0;  // of all matrices' rows
     int count, slot, matrix = 0;
     if (P.offsets) {
@@ -221,6 +222,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(Fp8QuantArgs P, 
         row0 = g.first + (int64_t)b * FP8_BLOCK;
     } else {
         matrix = at / slots;
+        if (matrix >= P.batch) return;
         slot = at - matrix * slots;
         count = (int)(P.rows - (int64_t)slot * FP8_BLOCK < FP8_BLOCK ? P.rows - (int64_t)slot * FP8_BLOCK : FP8_BLOCK);
         row0 = matrix * P.rows + (int64_t)slot * FP8_BLOCK;
@@ -295,13 +297,13 @@ static hipError_t launch(const Fp8QuantArgs &P, hipStream_t st)
         const int64_t rows = P.batch * P.rows, across = (tiles + 3) / 4;
         // few rows: one a group of lanes, so that more waves load
         const int rpg = STREAMED || rows * tiles >= 32 * 1024 ? 8 : 1;
-        const dim3 grid((unsigned)(across * ((rows + 4 * rpg - 1) / (4 * rpg))));
+        const dim3 grid = launch_grid(across * ((rows + 4 * rpg - 1) / (4 * rpg)));
         if (rpg == 8) fp8_quantize_rows_kernel<DT, STREAMED, 8><<<grid, 256, 0, st>>>(P, rows, (int)tiles, (unsigned)across);
         else fp8_quantize_rows_kernel<DT, false, 1><<<grid, 256, 0, st>>>(P, rows, (int)tiles, (unsigned)across);
         return hipGetLastError();
     }
     const int64_t slots = fp8_slots(P.rows, P.offsets ? P.groups : 0);
-    const dim3 grid((unsigned)(tiles * slots * P.batch));
+    const dim3 grid = launch_grid(tiles * slots * P.batch);
     if (P.codes_r) fp8_quantize_tile_kernel<DT, STREAMED, true><<<grid, 256, 0, st>>>(P, (int)tiles, (int)slots);
     else fp8_quantize_tile_kernel<DT, STREAMED, false><<<grid, 256, 0, st>>>(P, (int)tiles, (int)slots);
     return hipGetLastError();

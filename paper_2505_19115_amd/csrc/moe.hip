@@ -274,7 +274,7 @@ struct Piece {
 template <int G>
 __device__ __forceinline__ int64_t row_of()
 {
-    const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t wave = (int64_t)workgroup() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     return G == 64 ? wave : wave * (64 / G) + (threadIdx.x & 63) / G;
 }
 
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
     const int lane = threadIdx.x & (G - 1);
     const int64_t id = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (id >= pairs) {
-        const int64_t clearing = (int64_t)gridDim.x * (256 / G) - pairs;
+        const int64_t clearing = (int64_t)gridDim.x * gridDim.y * (256 / G) - pairs;
         for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
             walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
                 Piece<DT> v[U];
@@ -456,7 +456,7 @@ static int lanes_of(int64_t cols, int dt)
     return pieces <= 16 ? 8 : pieces <= 32 ? 16 : pieces <= 64 ? 32 : 64;
 }
 // (rows of a wave's groups of lanes)
-static dim3 grid_of(int64_t rows, int lanes) { return dim3((unsigned)((rows + 256 / lanes - 1) / (256 / lanes))); }
+static dim3 grid_of(int64_t rows, int lanes) { return launch_grid((rows + 256 / lanes - 1) / (256 / lanes)); }
 
 #define NVFP4_MOE_PICK(kernel, dt, s, lanes)                                                            \
     ((dt) == NVFP4_BF16 ? ((lanes) == 8 ? kernel<NVFP4_BF16, false, 8>                                  \
