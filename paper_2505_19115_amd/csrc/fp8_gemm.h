@@ -51,7 +51,7 @@ __device__ __forceinline__ RowTile row_tile(const int32_t *offsets, int groups, 
             a = a < 0 ? 0 : a > total ? total : a;
             b = b < a ? a : b > total ? total : b;
         }
-        const int mine = (b - a + step - 1) / step;
+        const int mine = (int)(((unsigned)(b - a) + (unsigned)step - 1) / (unsigned)step);  // (up to 2^31 - 1 rows)
         int upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {

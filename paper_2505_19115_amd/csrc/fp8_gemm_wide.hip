@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                     // tiles of the group before, which ends here
                     int before = __shfl_up(a, 1);
                     before = lane == 0 ? row : before;
-                    int n = e == 0 || e > groups ? 0 : (a - before + BM - 1) / BM;
+                    int n = e == 0 || e > groups ? 0 : (int)(((unsigned)(a - before) + BM - 1) / BM);  // (up to 2^31 - 1 rows)
 #pragma unroll
                     for (int d = 1; d < 64; d <<= 1) {
                         const int up = __shfl_up(n, d);

@@ -81,3 +81,13 @@ def test_products_without_a_contraction():
     del out
     offsets = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
     assert int(nv.fp8_gemm_experts(e4m3(1), e4m3(most), offsets).count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("kept", [(1 << 31) - 1, 5])
+def test_an_expert_of_the_most_rows(kept):
+    # a group's rows (an expert's, or those of none) and a tile's more than 32 bits hold with a sign
+    most = (1 << 31) - 1
+    out = torch.full((most, 1), 3.0, dtype=torch.bfloat16, device="cuda")
+    offsets = torch.tensor([0, kept], dtype=torch.int32, device="cuda")
+    assert nv.lib.nvfp4_fp8_gemm_experts(most, 1, 0, 1, offsets.data_ptr(), None, None, None, None, out.data_ptr(), nv.BF16, 1, torch.cuda.current_stream().cuda_stream) == nv.OK
+    assert int(out.count_nonzero()) == 0
