@@ -181,8 +181,12 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             const int row = __builtin_amdgcn_readfirstlane(group_row[e] + (ty - group_tile[e]) * BM), end = __builtin_amdgcn_readfirstlane(group_row[e + 1]);
             T.m0 = row;
             left = end - row;
-            if (e < P.groups) T.b0 = e * P.N;
-            else keep = 0;  // rows of no expert: zeros
+            if (e < P.groups) {
+                T.b0 = e * P.N;
+            } else {  // rows of no expert
+                keep = 0;
+                T.count = 1;
+            }
         } else {
             if (MODE == FP8_EXPERTS_DW) {
                 const int row = __builtin_amdgcn_readfirstlane(group_row[e]), rows = __builtin_amdgcn_readfirstlane(group_row[e + 1]) - row;
