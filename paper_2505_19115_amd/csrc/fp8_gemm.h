@@ -129,7 +129,7 @@ __device__ __forceinline__ uint32_t four_scales(const uint8_t *scales, int64_t r
         return w;
     }
     const int l = (int)left, from = 4 * c + 4 <= l ? 4 * c : l - 4, off = 4 * c - from;
-    return off >= 4 ? 0u : reinterpret_cast<const Four *>(p + from)->w >> (8 * off);
+    return off >= 4 ? 0x7F7F7F7Fu : reinterpret_cast<const Four *>(p + from)->w >> (8 * off);
 }
 
 // Two ways to multiply a K tile of two fragments of 16 rows, of which a lane holds 32 codes each.
@@ -141,14 +141,16 @@ __device__ __forceinline__ uint32_t four_scales(const uint8_t *scales, int64_t r
 //     are binary32 (1e-7 of the norm), at half the rate and for 32 conversions a lane.  That is exact for scale bytes LEAST .. MOST: below, the smallest codes
 //     need bits under bf16's least subnormal 2^-133, above, 448 * 2^(byte - 127) passes its largest number (a finite tensor's byte is 247 from
 //     1.75 * 2^127 on, torch.finfo(torch.bfloat16).min among them).  A wave that meets a block beyond these sums its outputs by multiply_codes().
-constexpr uint32_t LEAST = 3, MOST = 246;
+//     Bits are lost of the lower ones only against scale bytes above LARGE: against others a product is off by less than 2^-126, and blocks of zeros, which have byte 0,
+//     cost nothing.
+constexpr uint32_t LEAST = 3, MOST = 246, LARGE = 126;
 struct Codes {
     u32x4_t lo, hi;  // chunks q and q + 4 of a row's eight
     __device__ __forceinline__ bool any() const
     {
         return ((lo[0] | lo[1] | lo[2] | lo[3] | hi[0] | hi[1] | hi[2] | hi[3]) & 0x7F7F7F7Fu) != 0;
     }
-    // whether bf16 may not hold these codes with this scale (a block of zeros has byte 0, which costs nothing)
+    // whether bf16 may not hold these codes with this scale
     __device__ __forceinline__ bool beyond(uint32_t byte) const { return byte > MOST || (byte < LEAST && any()); }
     __device__ __forceinline__ int8v_t all() const
     {
@@ -160,28 +162,42 @@ struct Expanded {
     bf16x8_t v[4];
 };
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+// eight codes of step i of four
+__device__ __forceinline__ bf16x8_t expand(const Codes &x, float s, int i)
+{
+    bf16x8_t r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w = i < 2 ? x.lo[2 * i + h] : x.hi[2 * (i - 2) + h];
+        const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 1);
+        r[4 * h] = a[0];
+        r[4 * h + 1] = a[1];
+        r[4 * h + 2] = b[0];
+        r[4 * h + 3] = b[1];
+    }
+    return r;
+}
 __device__ __forceinline__ Expanded expand(const Codes &x, uint32_t byte)
 {
     const float s = scale_of(byte);
     Expanded r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t w = i < 2 ? x.lo[2 * i + h] : x.hi[2 * (i - 2) + h];
-            const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, 1);
-            r.v[i][4 * h] = a[0];
-            r.v[i][4 * h + 1] = a[1];
-            r.v[i][4 * h + 2] = b[0];
-            r.v[i][4 * h + 3] = b[1];
-        }
+    for (int i = 0; i < 4; ++i) r.v[i] = expand(x, s, i);
     return r;
 }
-// Whether one of four bytes is below LEAST or above MOST
-__device__ __forceinline__ bool odd_bytes(uint32_t v)
+// Whether one of eight scale bytes is outside 64 .. 191, that is has its two top bits alike: what few operations say of LEAST .. MOST
+__device__ __forceinline__ bool far_bytes(uint32_t a, uint32_t b) { return (~((a ^ (a << 1)) & (b ^ (b << 1))) & 0x80808080u) != 0; }
+__device__ __forceinline__ void extend(uint32_t &least, uint32_t &most, uint32_t byte)
 {
-    const uint32_t low = v & 0x7F7F7F7Fu, top = 0x80808080u, from_least = low + (0x80 - LEAST) * 0x01010101u, past_most = low + (0xFF - MOST) * 0x01010101u;
-    return ((~(v | from_least) | (v & past_most)) & top) != 0;
+    least = byte < least ? byte : least;
+    most = byte > most ? byte : most;
+}
+// Whether codes have to be looked at for blocks that bf16 does not hold: by the wave's scale bytes of both operands
+__device__ __forceinline__ bool suspects(uint32_t least_a, uint32_t most_a, uint32_t least_b, uint32_t most_b)
+{
+    const uint32_t least = least_a < least_b ? least_a : least_b, most = most_a > most_b ? most_a : most_b;
+    if (__builtin_expect(__ballot(least < LEAST || most > MOST) == 0, 1)) return false;
+    return __ballot(most > MOST) != 0 || (__ballot(least_a < LEAST) != 0 && __ballot(most_b > LARGE) != 0) || (__ballot(least_b < LEAST) != 0 && __ballot(most_a > LARGE) != 0);
 }
 // step i of four
 __device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, const Expanded &a, int i)
@@ -193,7 +209,7 @@ __device__ __forceinline__ void multiply(float4v_t &acc, const Expanded &b, cons
 __device__ __forceinline__ bool any_beyond(const uint8_t *codes, const uint8_t *scale, int64_t rows, int kt, int step, int end)
 {
     bool beyond = false;
-#pragma unroll 4
+#pragma unroll 2
     for (; kt < end; kt += step) {
         const Codes x = codes_at(codes + (int64_t)kt * KT);
         const uint32_t byte = scale[kt * rows];
@@ -209,11 +225,14 @@ __device__ __forceinline__ float4v_t multiply_codes(const Fp8GemmArgs &P, const 
     float4v_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (; kt < end; kt += step) {
-        const Expanded eb = expand(codes_at(b + (int64_t)kt * KT), 127), ea = expand(codes_at(a + (int64_t)kt * KT), 127);
+        const Codes xb = codes_at(b + (int64_t)kt * KT), xa = codes_at(a + (int64_t)kt * KT);
         const uint32_t mine = sb[kt * P.b_rows], s = sa[kt * P.a_rows];
         float4v_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) multiply(sum, eb, ea, i);
+        for (int i = 0; i < 4; ++i) {
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand(xb, 1.0f, i), expand(xa, 1.0f, i), sum, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);  // (registers of one step: the kernels' other paths are to have as many waves as without this one)
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t r = (uint32_t)__shfl((int)mine, 4 * (int)((threadIdx.x & 63) >> 4) + i);  // acc's rows of B: positions 4 q .. 4 q + 3

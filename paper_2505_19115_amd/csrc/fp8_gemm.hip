@@ -64,9 +64,6 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
 #pragma unroll
         for (int b = 0; b < 4; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
     const int ma = wm * 64 < T.rows ? wm * 64 : 0, nb = wn * 64 < T.cols ? wn * 64 : 0;  // (a wave past the edge computes what nobody stores)
-    // bytes of rows 4 c .. 4 c + 3 that are the tile's (four_scales())
-    auto bytes_of = [&](int rows) -> uint32_t { return rows >= 4 ? ~0u : rows > 0 ? (1u << (8 * rows)) - 1 : 0u; };
-    const uint32_t rows_a = bytes_of(T.rows - ma - 4 * c), rows_b = bytes_of(T.cols - nb - 4 * c);
     bool beyond = false;
     if (T.count > 0) {
         fetch(0);
@@ -85,11 +82,19 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
         };
         if constexpr (OUT_DT == NVFP4_F32) {
             // (blocks of the rows that there are)
-            if (__builtin_expect(__ballot(odd_bytes((sa & rows_a) | (~rows_a & 0x7F7F7F7Fu)) || odd_bytes((sb & rows_b) | (~rows_b & 0x7F7F7F7Fu))) != 0, 0)) {
+            if (__builtin_expect(__ballot(far_bytes(sa, sb)) != 0, 0)) {
+                uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    beyond |= ((rows_a >> (8 * j)) & 255) != 0 && read(A, j).beyond((sa >> (8 * j)) & 255);
-                    beyond |= ((rows_b >> (8 * j)) & 255) != 0 && read(B, j).beyond((sb >> (8 * j)) & 255);
+                    if (4 * c + j < T.rows - ma) extend(least_a, most_a, (sa >> (8 * j)) & 255);
+                    if (4 * c + j < T.cols - nb) extend(least_b, most_b, (sb >> (8 * j)) & 255);
+                }
+                if (suspects(least_a, most_a, least_b, most_b)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        beyond |= 4 * c + j < T.rows - ma && read(A, j).beyond((sa >> (8 * j)) & 255);
+                        beyond |= 4 * c + j < T.cols - nb && read(B, j).beyond((sb >> (8 * j)) & 255);
+                    }
                 }
             }
             Expanded fa[4];

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
     for (int a = 0; a < MT; ++a)
 #pragma unroll
         for (int b = 0; b < TN; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-    bool odd = false;  // (binary32 outputs) a scale byte of a block that bf16 may not hold
+    uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;  // (binary32 outputs) scale bytes
     for (int kt = wave; kt < T.count; kt += NW * U) {
         Codes fb[U][TN], fa[U][MT];
         uint32_t sb[U][TN], sa[U][MT];
@@ -92,15 +92,15 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
-                for (int a = 0; a < MT; ++a) odd |= sa[u][a] - LEAST > MOST - LEAST;
+                for (int a = 0; a < MT; ++a) extend(least_a, most_a, sa[u][a]);
 #pragma unroll
-                for (int b = 0; b < TN; ++b) odd |= sb[u][b] - LEAST > MOST - LEAST;
+                for (int b = 0; b < TN; ++b) extend(least_b, most_b, sb[u][b]);
             }
         }
     }
     // blocks that bf16 does not hold, or of zeros: which, from memory (looked at above, codes would stay in registers longer)
     bool beyond = false;
-    if (OUT_DT == NVFP4_F32 && __builtin_expect(__ballot(odd) != 0, 0)) {
+    if (OUT_DT == NVFP4_F32 && __builtin_expect(suspects(least_a, most_a, least_b, most_b), 0)) {
 #pragma unroll 1
         for (int f = 0; f < MT + TN; ++f) {
             const int r = 16 * (f < MT ? f : f - MT) + c;

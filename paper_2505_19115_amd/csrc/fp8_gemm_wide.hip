@@ -369,14 +369,12 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                 };
                 // Blocks that bf16 does not hold, in a tile with scale bytes that may be such.  (A0 and P are in registers, and their places others' to write; Q and A1
                 // stay until the barrier.)
-                uint32_t least = ~0u, most = 0;
+                uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;
 #pragma unroll
-                for (int f = 0; f < 8 + FB; ++f) {
-                    const uint32_t byte = f < 8 ? SA[ST][f >> 2][f & 3] : SB[ST][(f - 8) >> 2][f & 3];
-                    least = byte < least ? byte : least;
-                    most = byte > most ? byte : most;
-                }
-                if (__builtin_expect(__ballot(least < LEAST || most > MOST) != 0, 0)) {
+                for (int f = 0; f < 8; ++f) extend(least_a, most_a, SA[ST][f >> 2][f & 3]);
+#pragma unroll
+                for (int f = 0; f < FB; ++f) extend(least_b, most_b, SB[ST][f >> 2][f & 3]);
+                if (__builtin_expect(suspects(least_a, most_a, least_b, most_b), 0)) {
                     auto there = [&](const uint8_t *const (&base)[2], int f) -> Codes {
                         return {*reinterpret_cast<const u32x4_t *>(base[0] + 16 * f * KT), *reinterpret_cast<const u32x4_t *>(base[1] + 16 * f * KT)};
                     };

@@ -129,3 +129,13 @@ def test_blocks_of_zeros_change_no_other_row(M, N, K, dtype):
     a.scales[:, rows] = 0
     out = nv.fp8_gemm(a, b, out_dtype=dtype)
     assert bool((out[rows] == 0).all()) and torch.equal(out[~rows], ref[~rows])
+
+
+@pytest.mark.parametrize("M, N, K", SIZES)
+def test_the_least_tensors_against_ordinary_ones(M, N, K):
+    # of blocks under 2^-118, whose codes pass bf16's least, a product with magnitudes up to 224 may be off by 2^-126
+    g = torch.Generator(device="cuda").manual_seed(M + 2 * N)
+    a, b = operand(g, M, K, (0, 1, 2, 120)), operand(g, N, K, (110, 120, 126))
+    out, A, B = nv.fp8_gemm(a, b, out_dtype=torch.float32), values(a), values(b)
+    most = (K / 32 + K / 128 + 48) * (2.0 ** -24 * (A.abs() @ B.abs().t()) + 2.0 ** -149) + K * 2.0 ** -126
+    assert bool(((out.double() - A @ B.t()).abs() <= most).all())
