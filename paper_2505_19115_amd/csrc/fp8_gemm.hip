@@ -173,11 +173,12 @@ static double thin_cost(const Fp8GemmArgs &P, int out_dt) { return fp8_gemm_thin
 
 // Parts of the contraction of a dense product (1: not divided), where that is quicker than every kernel that does not divide it (3 and 2.5 us: their start) by more
 // than the host takes for the second launch: 16 x 64 x 12288 and 64 x 128 x 12288 would gain 1 us of 13 on the GPU alone.
+// us, binary32, whole / divided: 384 x 6016 x 7296 75 / 62, 200 x 5000 x 4096 31 / 26, 777 x 1025 x 8192 34 / 32, 512 x 1000 x 8064 25.6 / 26.1.
 constexpr double SECOND_LAUNCH = 3.0;
 static int parts_of(const Fp8GemmArgs &P, int out_dt, size_t *bytes)
 {
     if (P.M > 0 && P.N > 0 && P.blocks > 0) {
-        const double tiles = tiles_cost(f8g::tiles<FP8_DENSE>(P, 128, 128), out_dt) * P.blocks + 3.0, thin = fp8_gemm_thin_cost(P) * P.blocks + 2.5;
+        const double tiles = tiles_cost(f8g::tiles<FP8_DENSE>(P, 128, 128), out_dt) * P.blocks + 3.0, thin = thin_cost(P, out_dt) * P.blocks + 2.5;
         const double whole = tiles < thin ? tiles : thin;
         double cost;
         const int parts = fp8_gemm_parts(P, out_dt, whole - SECOND_LAUNCH, bytes, &cost);
