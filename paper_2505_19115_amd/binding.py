@@ -753,7 +753,7 @@ def fp8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, order: 
         pitch, ld, lane = x.stride()
         if n <= 1:
             ld = pitch if batch > 1 else c
-        if batch > 1 and pitch != n * ld:
+        if batch > 1 and n > 0 and c > 0 and pitch != n * ld:
             raise ValueError("x: matrices one behind the other")
     else:
         raise ValueError("x: a matrix, or a stack of them without order and offsets")
