@@ -515,16 +515,23 @@ nvfp4_status nvfp4_moe_gather(const void *x, nvfp4_dtype dt, int64_t x_rows, int
                               int32_t top_k, int64_t rows, void *out, void *stream);
 /*
  * out[t] = sum_j weights[t, j] y[position[t, j]] over the choices that were not dropped, in their order, in binary32;
- * y [rows, cols], out [tokens, cols] dense, of dt.  weights: device fp32 [tokens, top_k], or NULL for ones (the
- * gradient of nvfp4_moe_gather).  A token without a choice gets zeros.
+ * y [rows, cols] of dt, out [tokens, cols] of out_dt, dense.  weights: device fp32 [tokens, top_k], or NULL for ones (the
+ * gradient of nvfp4_moe_gather).  A token without a choice gets zeros.  An experts' product that leaves binary32 rows is
+ * rounded once, here; bf16 rows are rounded on their own before they are summed.  nvfp4_moe_combine: out in y's type.
  */
+nvfp4_status nvfp4_moe_combine_to(const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols, const float *weights,
+                                  const int32_t *position, int64_t tokens, int32_t top_k, void *out, nvfp4_dtype out_dt,
+                                  void *stream);
 nvfp4_status nvfp4_moe_combine(const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols, const float *weights,
                                const int32_t *position, int64_t tokens, int32_t top_k, void *out, void *stream);
 /*
- * Its gradient for the upstream dout [tokens, cols]: dy[position[t, j]] = weights[t, j] dout[t] and dweights[t, j] =
- * dout[t] . y[position[t, j]] (binary32; 0 for a dropped pair).  offsets: of the sort, [groups + 1]; rows of dy past
- * the last kept pair are set to zero.  dy must not share memory with y.
+ * Its gradient for the upstream dout [tokens, cols] of dout_dt (nvfp4_moe_combine_bwd: y's type): dy[position[t, j]] =
+ * weights[t, j] dout[t] in y's type, and dweights[t, j] = dout[t] . y[position[t, j]] (binary32; 0 for a dropped pair).
+ * offsets: of the sort, [groups + 1]; rows of dy past the last kept pair are set to zero.  dy must not share memory with y.
  */
+nvfp4_status nvfp4_moe_combine_to_bwd(const void *dout, nvfp4_dtype dout_dt, const void *y, nvfp4_dtype dt, int64_t rows,
+                                      int64_t cols, const float *weights, const int32_t *position, const int32_t *offsets,
+                                      int32_t groups, int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream);
 nvfp4_status nvfp4_moe_combine_bwd(const void *dout, const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols,
                                    const float *weights, const int32_t *position, const int32_t *offsets, int32_t groups,
                                    int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream);

@@ -180,8 +180,12 @@ def _load() -> C.CDLL:
     L.nvfp4_moe_gather.argtypes = [vp, ci, i64, i64, i64, vp, i32, i64, vp, vp]
     L.nvfp4_moe_combine.restype = ci
     L.nvfp4_moe_combine.argtypes = [vp, ci, i64, i64, vp, vp, i64, i32, vp, vp]
+    L.nvfp4_moe_combine_to.restype = ci
+    L.nvfp4_moe_combine_to.argtypes = [vp, ci, i64, i64, vp, vp, i64, i32, vp, ci, vp]
     L.nvfp4_moe_combine_bwd.restype = ci
     L.nvfp4_moe_combine_bwd.argtypes = [vp, vp, ci, i64, i64, vp, vp, vp, i32, i64, i32, vp, vp, vp]
+    L.nvfp4_moe_combine_to_bwd.restype = ci
+    L.nvfp4_moe_combine_to_bwd.argtypes = [vp, ci, vp, ci, i64, i64, vp, vp, vp, i32, i64, i32, vp, vp, vp]
     L.nvfp4_probe_mfma_rate.restype = C.c_int
     L.nvfp4_probe_mfma_rate.argtypes = [C.c_int, C.c_int, C.c_int, vp, C.c_size_t, C.POINTER(C.c_double), vp]
     return L
@@ -219,6 +223,7 @@ EXPORTS = (
     "nvfp4_swiglu_bwd_workspace_bytes", "nvfp4_swiglu_bwd_quantize", "nvfp4_linear_bwd_dyq", "nvfp4_host_swiglu_bwd", "nvfp4_swiglu_bwd",
     "nvfp4_fp8_codes_bytes", "nvfp4_fp8_scales_bytes", "nvfp4_fp8_slots", "nvfp4_fp8_quantize", "nvfp4_fp8_gemm", "nvfp4_fp8_gemm_workspace_bytes", "nvfp4_fp8_gemm_ws", "nvfp4_fp8_gemm_experts",
     "nvfp4_fp8_gemm_experts_dw", "nvfp4_moe_sort_workspace_bytes", "nvfp4_moe_sort", "nvfp4_moe_gather", "nvfp4_moe_combine", "nvfp4_moe_combine_bwd",
+    "nvfp4_moe_combine_to", "nvfp4_moe_combine_to_bwd",
 )
 
 
@@ -886,32 +891,33 @@ def _routing(position: torch.Tensor, weights: torch.Tensor | None) -> tuple[int,
     return p_position, weights.data_ptr()
 
 
-def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None = None) -> torch.Tensor:
-    """nvfp4_moe_combine: y [pairs, D], position [T, top_k] -> [T, D] = sum_j weights[t, j] y[position[t, j]]; without weights the plain sum,
-    which is moe_gather's gradient."""
+def moe_combine(y: torch.Tensor, position: torch.Tensor, weights: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """nvfp4_moe_combine_to: y [pairs, D], position [T, top_k] -> [T, D] = sum_j weights[t, j] y[position[t, j]] in out_dtype (y's where left out); without
+    weights the plain sum, which is moe_gather's gradient.  A product's binary32 rows are rounded to bf16 once this way."""
     _require_gpu(y)
     p_position, p_weights = _routing(position, weights)
     if y.dim() != 2 or not y.is_contiguous():
         raise ValueError("y: a dense matrix")
     (R, D), (T, k) = y.shape, position.shape
-    out = torch.empty(T, D, dtype=y.dtype, device=y.device)
-    code = lib.nvfp4_moe_combine(y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, T, k, out.data_ptr(), _stream())
+    out = torch.empty(T, D, dtype=out_dtype or y.dtype, device=y.device)
+    code = lib.nvfp4_moe_combine_to(y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, T, k, out.data_ptr(), _dtype_tag(out), _stream())
     if code:
-        _check(code, "nvfp4_moe_combine")
+        _check(code, "nvfp4_moe_combine_to")
     return out
 
 
 def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, weights: torch.Tensor, position: torch.Tensor,
-                    offsets: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
-    """nvfp4_moe_combine_bwd: the gradient of moe_combine(y, position, weights) for dout [T, D] -> (dy like y, dweights float32 like weights)."""
+                    offsets: torch.Tensor, out_dtype: torch.dtype | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """nvfp4_moe_combine_to_bwd: the gradient of moe_combine(y, position, weights, out_dtype) for dout [T, D], of that type -> (dy like y, dweights float32 like
+    weights)."""
     _require_gpu(dout, y)
     p_offsets, (p_position, p_weights) = _int32(offsets, "offsets"), _routing(position, weights)
-    if y.dim() != 2 or not y.is_contiguous() or not dout.is_contiguous() or dout.dtype is not y.dtype or dout.shape != (position.shape[0], y.shape[1]):
-        raise ValueError("y: a dense matrix; dout: dense [T, D] of its type")
+    if y.dim() != 2 or not y.is_contiguous() or not dout.is_contiguous() or dout.dtype is not (out_dtype or y.dtype) or dout.shape != (position.shape[0], y.shape[1]):
+        raise ValueError("y: a dense matrix; dout: dense [T, D] of its type, or of out_dtype")
     (R, D), (T, k) = y.shape, position.shape
     dy, dweights = torch.empty_like(y), torch.empty_like(weights)
-    code = lib.nvfp4_moe_combine_bwd(dout.data_ptr(), y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, p_offsets, offsets.numel() - 1, T, k,
-                                     dy.data_ptr(), dweights.data_ptr(), _stream())
+    code = lib.nvfp4_moe_combine_to_bwd(dout.data_ptr(), _dtype_tag(dout), y.data_ptr(), _dtype_tag(y), R, D, p_weights, p_position, p_offsets, offsets.numel() - 1, T, k,
+                                        dy.data_ptr(), dweights.data_ptr(), _stream())
     if code:
-        _check(code, "nvfp4_moe_combine_bwd")
+        _check(code, "nvfp4_moe_combine_to_bwd")
     return dy, dweights

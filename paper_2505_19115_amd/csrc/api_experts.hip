@@ -185,32 +185,46 @@ nvfp4_status nvfp4_moe_gather(const void *x, nvfp4_dtype dt_, int64_t x_rows, in
     return done(launch_moe_gather(x, dt, x_rows, cols, ld, order, top_k, rows, out, reinterpret_cast<hipStream_t>(stream)));
 }
 
-nvfp4_status nvfp4_moe_combine(const void *y, nvfp4_dtype dt_, int64_t rows, int64_t cols, const float *weights,
-                               const int32_t *position, int64_t tokens, int32_t top_k, void *out, void *stream)
+nvfp4_status nvfp4_moe_combine_to(const void *y, nvfp4_dtype dt_, int64_t rows, int64_t cols, const float *weights,
+                                  const int32_t *position, int64_t tokens, int32_t top_k, void *out, nvfp4_dtype out_dt_,
+                                  void *stream)
 {
-    const int dt = raw(dt_);
-    if (!valid_dtype(dt) || top_k < 1) return NVFP4_EINVAL;
+    const int dt = raw(dt_), out_dt = raw(out_dt_);
+    if (!valid_dtype(dt) || !valid_dtype(out_dt) || top_k < 1) return NVFP4_EINVAL;
     if (rows < 0 || rows > MOST_ROWS || cols < 0 || tokens < 0 || tokens > MOST_ROWS / top_k) return NVFP4_ESHAPE;
     if (tokens == 0 || cols == 0) return NVFP4_OK;
     if ((!y && rows > 0) || !position || !out) return NVFP4_EINVAL;
-    if (!aligned(y, elem(dt)) || !aligned(out, elem(dt)) || !aligned(position, 4) || !aligned(weights, 4)) return NVFP4_EALIGN;
-    return done(launch_moe_combine(y, dt, rows, cols, weights, position, tokens, top_k, out, reinterpret_cast<hipStream_t>(stream)));
+    if (!aligned(y, elem(dt)) || !aligned(out, elem(out_dt)) || !aligned(position, 4) || !aligned(weights, 4)) return NVFP4_EALIGN;
+    return done(launch_moe_combine(y, dt, rows, cols, weights, position, tokens, top_k, out, out_dt, reinterpret_cast<hipStream_t>(stream)));
 }
 
-nvfp4_status nvfp4_moe_combine_bwd(const void *dout, const void *y, nvfp4_dtype dt_, int64_t rows, int64_t cols,
-                                   const float *weights, const int32_t *position, const int32_t *offsets, int32_t groups,
-                                   int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream)
+nvfp4_status nvfp4_moe_combine(const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols, const float *weights,
+                               const int32_t *position, int64_t tokens, int32_t top_k, void *out, void *stream)
 {
-    const int dt = raw(dt_);
-    if (!valid_dtype(dt) || top_k < 1 || groups < 1 || groups > MAX_EXPERTS) return NVFP4_EINVAL;
+    return nvfp4_moe_combine_to(y, dt, rows, cols, weights, position, tokens, top_k, out, dt, stream);
+}
+
+nvfp4_status nvfp4_moe_combine_to_bwd(const void *dout, nvfp4_dtype dout_dt_, const void *y, nvfp4_dtype dt_, int64_t rows,
+                                      int64_t cols, const float *weights, const int32_t *position, const int32_t *offsets,
+                                      int32_t groups, int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream)
+{
+    const int dt = raw(dt_), dout_dt = raw(dout_dt_);
+    if (!valid_dtype(dt) || !valid_dtype(dout_dt) || top_k < 1 || groups < 1 || groups > MAX_EXPERTS) return NVFP4_EINVAL;
     if (rows < 0 || rows > MOST_ROWS || cols < 0 || tokens < 0 || tokens > MOST_ROWS / top_k) return NVFP4_ESHAPE;
     if (tokens == 0 && (rows == 0 || cols == 0)) return NVFP4_OK;
     if (!offsets || (tokens > 0 && (!weights || !position || !dweights)) || (cols > 0 && ((tokens > 0 && !dout) || (rows > 0 && (!y || !dy))))) return NVFP4_EINVAL;
-    if (!aligned(dout, elem(dt)) || !aligned(y, elem(dt)) || !aligned(dy, elem(dt)) || !aligned(weights, 4) || !aligned(position, 4) || !aligned(offsets, 4) ||
+    if (!aligned(dout, elem(dout_dt)) || !aligned(y, elem(dt)) || !aligned(dy, elem(dt)) || !aligned(weights, 4) || !aligned(position, 4) || !aligned(offsets, 4) ||
         !aligned(dweights, 4))
         return NVFP4_EALIGN;
-    return done(launch_moe_combine_bwd(dout, y, dt, rows, cols, weights, position, offsets + groups, tokens, top_k, dy, dweights,
+    return done(launch_moe_combine_bwd(dout, dout_dt, y, dt, rows, cols, weights, position, offsets + groups, tokens, top_k, dy, dweights,
                                        reinterpret_cast<hipStream_t>(stream)));
+}
+
+nvfp4_status nvfp4_moe_combine_bwd(const void *dout, const void *y, nvfp4_dtype dt, int64_t rows, int64_t cols,
+                                   const float *weights, const int32_t *position, const int32_t *offsets, int32_t groups,
+                                   int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream)
+{
+    return nvfp4_moe_combine_to_bwd(dout, dt, y, dt, rows, cols, weights, position, offsets, groups, tokens, top_k, dy, dweights, stream);
 }
 
 }  // extern "C"

@@ -99,8 +99,8 @@ hipError_t launch_moe_sort(const void *experts, int id_bytes, int64_t pairs, int
 hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out,
                              hipStream_t st);
 hipError_t launch_moe_combine(const void *y, int dt, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position, int64_t tokens,
-                              int32_t top_k, void *out, hipStream_t st);
-hipError_t launch_moe_combine_bwd(const void *dout, const void *y, int dt, int64_t rows, int64_t cols, const float *weights, const int32_t *position,
+                              int32_t top_k, void *out, int out_dt, hipStream_t st);
+hipError_t launch_moe_combine_bwd(const void *dout, int dout_dt, const void *y, int dt, int64_t rows, int64_t cols, const float *weights, const int32_t *position,
                                   const int32_t *kept, int64_t tokens, int32_t top_k, void *dy, float *dweights, hipStream_t st);
 
 }  // namespace nvfp4

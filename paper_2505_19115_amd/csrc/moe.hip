@@ -214,32 +214,39 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float float2v_t __attribute__((ext_vector_type(2)));
 
-// 16 bytes of a row at any element
-template <int DT>
+// Elements that fill 16 bytes of a row of a type; beside a narrower one, as many as it has
+constexpr int per_piece(int dt) { return dt == NVFP4_BF16 ? 8 : 4; }
+
+// N neighbouring elements of a row, from any element on
+template <int DT, int N = per_piece(DT)>
 struct Piece {
-    static constexpr int N = DT == NVFP4_BF16 ? 8 : 4, ESZ = DT == NVFP4_BF16 ? 2 : 4;
-    struct __attribute__((packed, aligned(2))) P2 { u32x4_t w; };
-    struct __attribute__((packed, aligned(4))) P4 { u32x4_t w; };
-    u32x4_t w;
+    static constexpr int ESZ = DT == NVFP4_BF16 ? 2 : 4, W = N * ESZ / 16;
+    struct __attribute__((packed, aligned(ESZ))) P { u32x4_t w; };
+    u32x4_t w[W];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[k] = u32x4_t{0, 0, 0, 0};
+    }
     template <bool STREAMED>
     __device__ __forceinline__ void load(const uint8_t *p)
     {
-        if (STREAMED) w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
-        else w = DT == NVFP4_BF16 ? reinterpret_cast<const P2 *>(p)->w : reinterpret_cast<const P4 *>(p)->w;
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[k] = STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p) + k) : reinterpret_cast<const P *>(p)[k].w;
     }
     __device__ __forceinline__ void store(uint8_t *p) const
     {
-        if (DT == NVFP4_BF16) reinterpret_cast<P2 *>(p)->w = w;
-        else reinterpret_cast<P4 *>(p)->w = w;
+#pragma unroll
+        for (int k = 0; k < W; ++k) reinterpret_cast<P *>(p)[k].w = w[k];
     }
     __device__ __forceinline__ void load_some(const uint8_t *p, int n)
     {
-        w = u32x4_t{0, 0, 0, 0};
+        zero();
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < n) {
-                if (DT == NVFP4_BF16) w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i & 1));
-                else w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+                if (DT == NVFP4_BF16) w[0][(i >> 1) & 3] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << (16 * (i & 1));
+                else w[(i >> 2) % W][i & 3] = reinterpret_cast<const uint32_t *>(p)[i];
             }
     }
     __device__ __forceinline__ void store_some(uint8_t *p, int n) const
@@ -247,13 +254,13 @@ struct Piece {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < n) {
-                if (DT == NVFP4_BF16) reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-                else reinterpret_cast<uint32_t *>(p)[i] = w[i];
+                if (DT == NVFP4_BF16) reinterpret_cast<uint16_t *>(p)[i] = (uint16_t)(w[0][(i >> 1) & 3] >> (16 * (i & 1)));
+                else reinterpret_cast<uint32_t *>(p)[i] = w[(i >> 2) % W][i & 3];
             }
     }
     __device__ __forceinline__ float get(int i) const
     {
-        return DT == NVFP4_BF16 ? __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16) : __uint_as_float(w[i & 3]);
+        return DT == NVFP4_BF16 ? __uint_as_float(i & 1 ? w[0][(i >> 1) & 3] & 0xFFFF0000u : w[0][(i >> 1) & 3] << 16) : __uint_as_float(w[(i >> 2) % W][i & 3]);
     }
     __device__ __forceinline__ void set(const float (&v)[N])
     {
@@ -261,11 +268,11 @@ struct Piece {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2v_t f = {v[(2 * i) % N], v[(2 * i + 1) % N]};
-                w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+                w[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+            for (int i = 0; i < N; ++i) w[(i >> 2) % W][i & 3] = __float_as_uint(v[i]);
         }
     }
 };
@@ -278,12 +285,11 @@ __device__ __forceinline__ int64_t row_of()
     return G == 64 ? wave : wave * (64 / G) + (threadIdx.x & 63) / G;
 }
 
-// Walks a row in steps of U pieces a lane: body(at, n, again, whole) with the byte offsets of a lane's pieces, how many elements each has there (0: none), how many of
+// Walks a row in steps of U pieces of N elements a lane: body(at, n, again, whole) with the first elements of a lane's pieces, how many each has there (0: none), how many of
 // them the piece before has too (a row's last piece ends with the row), and whether all pieces are there and none overlaps, which is the same in the wave.
-template <int DT, int U, int G, class F>
+template <int N, int U, int G, class F>
 __device__ __forceinline__ void walk(int64_t cols, F &&body)
 {
-    constexpr int N = Piece<DT>::N;
     const int lane = threadIdx.x & (G - 1);
     for (int64_t c0 = 0; c0 < cols; c0 += G * N * U) {
         int64_t at[U];
@@ -293,30 +299,32 @@ __device__ __forceinline__ void walk(int64_t cols, F &&body)
             const int64_t c = c0 + (u * G + lane) * N;
             const int left = cols - c < N ? (int)(cols - c) : N;
             again[u] = left > 0 && cols >= N ? N - left : 0;
-            at[u] = (c - again[u]) * Piece<DT>::ESZ;
+            at[u] = c - again[u];
             n[u] = left > 0 ? left + again[u] : 0;
         }
         if (c0 + G * N * U <= cols) body(at, n, again, std::true_type{});
         else body(at, n, again, std::false_type{});
     }
 }
-template <int DT, bool WHOLE, bool STREAMED, int U>
-__device__ __forceinline__ void load(Piece<DT> (&v)[U], const uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
+template <bool WHOLE, bool STREAMED, int DT, int N, int U>
+__device__ __forceinline__ void load(Piece<DT, N> (&v)[U], const uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
 {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (WHOLE || n[u] == Piece<DT>::N) v[u].template load<STREAMED>(row + at[u]);
-        else if (n[u] > 0) v[u].load_some(row + at[u], n[u]);
-        else v[u].w = u32x4_t{0, 0, 0, 0};
+        const uint8_t *const p = row + at[u] * Piece<DT, N>::ESZ;
+        if (WHOLE || n[u] == N) v[u].template load<STREAMED>(p);
+        else if (n[u] > 0) v[u].load_some(p, n[u]);
+        else v[u].zero();
     }
 }
-template <int DT, bool WHOLE, int U>
-__device__ __forceinline__ void store(const Piece<DT> (&v)[U], uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
+template <bool WHOLE, int DT, int N, int U>
+__device__ __forceinline__ void store(const Piece<DT, N> (&v)[U], uint8_t *row, const int64_t (&at)[U], const int (&n)[U])
 {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (WHOLE || n[u] == Piece<DT>::N) v[u].store(row + at[u]);
-        else if (n[u] > 0) v[u].store_some(row + at[u], n[u]);
+        uint8_t *const p = row + at[u] * Piece<DT, N>::ESZ;
+        if (WHOLE || n[u] == N) v[u].store(p);
+        else if (n[u] > 0) v[u].store_some(p, n[u]);
     }
 }
 
@@ -334,37 +342,37 @@ __global__ __launch_bounds__(256) void moe_gather_kernel(const uint8_t *x, int64
     const int64_t src = pair < 0 || pair / top_k >= x_rows ? -1 : pair / top_k;
     const uint8_t *const from = x + src * ld * Piece<DT>::ESZ;
     uint8_t *const to = out + r * cols * Piece<DT>::ESZ;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
+    walk<per_piece(DT), U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         Piece<DT> v[U];
         if (src >= 0) {
-            load<DT, W, STREAMED>(v, from, at, n);
+            load<W, STREAMED>(v, from, at, n);
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
+            for (int u = 0; u < U; ++u) v[u].zero();
         }
-        store<DT, W>(v, to, at, n);
+        store<W>(v, to, at, n);
     });
 }
 
-// G lanes for each token.  Two choices at a time: as many loads in flight.
-template <int DT, bool STREAMED, int G>
+// G lanes for each token.  Two choices at a time: as many loads in flight.  DT: of y; OUT: of the result.
+template <int DT, int OUT, bool STREAMED, int G>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position,
                                                           int64_t tokens, int32_t top_k, uint8_t *out)
 {
     using namespace moe;
-    constexpr int U = 2, N = Piece<DT>::N;
+    constexpr int U = 2, N = per_piece(DT) > per_piece(OUT) ? per_piece(DT) : per_piece(OUT);
     const int64_t t = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (t >= tokens) return;
     const int32_t *const places = position + t * top_k;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
+    walk<N, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
         float sum[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[u][i] = 0.0f;
-        auto add = [&](const Piece<DT> (&v)[U], float w) {
+        auto add = [&](const Piece<DT, N> (&v)[U], float w) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -373,37 +381,37 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const uint8_t *y, int6
         for (int j = 0; j < top_k; j += 2) {
             const int32_t p = places[j], q = j + 1 < top_k ? places[j + 1] : -1;
             const bool has_p = p >= 0 && p < y_rows, has_q = q >= 0 && q < y_rows;
-            Piece<DT> a[U], b[U];
-            if (has_p) load<DT, W, STREAMED>(a, y + p * row, at, n);
-            if (has_q) load<DT, W, STREAMED>(b, y + q * row, at, n);
+            Piece<DT, N> a[U], b[U];
+            if (has_p) load<W, STREAMED>(a, y + p * row, at, n);
+            if (has_q) load<W, STREAMED>(b, y + q * row, at, n);
             if (has_p) add(a, weights ? weights[t * top_k + j] : 1.0f);
             if (has_q) add(b, weights ? weights[t * top_k + j + 1] : 1.0f);
         }
-        Piece<DT> v[U];
+        Piece<OUT, N> v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) v[u].set(sum[u]);
-        store<DT, W>(v, out + t * row, at, n);
+        store<W>(v, out + t * cols * Piece<OUT>::ESZ, at, n);
     });
 }
 
-// G lanes for each pair; behind them those that clear the rows of dy past the last kept pair
-template <int DT, bool STREAMED, int G>
+// G lanes for each pair; behind them those that clear the rows of dy past the last kept pair.  DT: of y and dy; UP: of dout.
+template <int DT, int UP, bool STREAMED, int G>
 __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dout, const uint8_t *y, int64_t rows, int64_t cols, const float *weights,
                                                               const int32_t *position, const int32_t *kept, int64_t pairs, int32_t top_k, uint8_t *dy,
                                                               float *dweights)
 {
     using namespace moe;
-    constexpr int U = 2, N = Piece<DT>::N;
+    constexpr int U = 2, N = per_piece(DT) > per_piece(UP) ? per_piece(DT) : per_piece(UP);
     const int lane = threadIdx.x & (G - 1);
     const int64_t id = row_of<G>(), row = cols * Piece<DT>::ESZ;
     if (id >= pairs) {
         const int64_t clearing = (int64_t)gridDim.x * gridDim.y * (256 / G) - pairs;
         for (int64_t r = (kept[0] < 0 ? 0 : kept[0]) + (id - pairs); r < rows; r += clearing)
-            walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
-                Piece<DT> v[U];
+            walk<N, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
+                Piece<DT, N> v[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) v[u].w = u32x4_t{0, 0, 0, 0};
-                store<DT, decltype(whole)::value>(v, dy + r * row, at, n);
+                for (int u = 0; u < U; ++u) v[u].zero();
+                store<decltype(whole)::value>(v, dy + r * row, at, n);
             });
         return;
     }
@@ -412,15 +420,16 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
         if (lane == 0) dweights[id] = 0.0f;
         return;
     }
-    const uint8_t *const up = dout + id / top_k * row, *const from = y + p * row;
+    const uint8_t *const up = dout + id / top_k * cols * Piece<UP>::ESZ, *const from = y + p * row;
     uint8_t *const to = dy + p * row;
     const float w = weights[id];
     float dot = 0.0f;
-    walk<DT, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
+    walk<N, U, G>(cols, [&](const int64_t (&at)[U], const int (&n)[U], const int (&again)[U], auto whole) {
         constexpr bool W = decltype(whole)::value;
-        Piece<DT> a[U], b[U];
-        load<DT, W, false>(a, up, at, n);
-        load<DT, W, STREAMED>(b, from, at, n);
+        Piece<UP, N> a[U];
+        Piece<DT, N> b[U];
+        load<W, false>(a, up, at, n);
+        load<W, STREAMED>(b, from, at, n);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[N];
@@ -429,9 +438,9 @@ __global__ __launch_bounds__(256) void moe_combine_bwd_kernel(const uint8_t *dou
                 v[i] = w * a[u].get(i);
                 if (W || i >= again[u]) dot = __builtin_fmaf(a[u].get(i), b[u].get(i), dot);
             }
-            a[u].set(v);
+            b[u].set(v);
         }
-        store<DT, W>(a, to, at, n);
+        store<W>(b, to, at, n);
     });
 #pragma unroll
     for (int d = G / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
@@ -450,58 +459,80 @@ static bool streams(const void *rows, int64_t n, int64_t cols, int dt)
 
 // Lanes of a row, which has two pieces for each at a time: short rows by a wave each are bound by how fast waves begin.  us, 64 lanes / so, 10010 tokens x 6 gathered, combined,
 // gradient: 64 bf16 20.4 / 7.0, 14.2 / 7.0, 28.6 / 9.5; 256 20.6 / 10.2, 15.0 / 8.3, 28.7 / 12.4; 512 20.0 / 18.4, 16.0 / 12.5, 31.2 / 25.0.
-static int lanes_of(int64_t cols, int dt)
+static int lanes_of(int64_t cols, int per_piece)
 {
-    const int64_t pieces = (cols * (dt == NVFP4_BF16 ? 2 : 4) + 15) / 16;
+    const int64_t pieces = (cols + per_piece - 1) / per_piece;
     return pieces <= 16 ? 8 : pieces <= 32 ? 16 : pieces <= 64 ? 32 : 64;
 }
 // (rows of a wave's groups of lanes)
 static dim3 grid_of(int64_t rows, int lanes) { return launch_grid((rows + 256 / lanes - 1) / (256 / lanes)); }
 
-#define NVFP4_MOE_PICK(kernel, dt, s, lanes)                                                            \
-    ((dt) == NVFP4_BF16 ? ((lanes) == 8 ? kernel<NVFP4_BF16, false, 8>                                  \
-                           : (lanes) == 16 ? kernel<NVFP4_BF16, false, 16>                              \
-                           : (lanes) == 32 ? kernel<NVFP4_BF16, false, 32>                              \
-                           : (s) ? kernel<NVFP4_BF16, true, 64> : kernel<NVFP4_BF16, false, 64>)        \
-                        : ((lanes) == 8 ? kernel<NVFP4_F32, false, 8>                                   \
-                           : (lanes) == 16 ? kernel<NVFP4_F32, false, 16>                               \
-                           : (lanes) == 32 ? kernel<NVFP4_F32, false, 32>                               \
-                           : (s) ? kernel<NVFP4_F32, true, 64> : kernel<NVFP4_F32, false, 64>))
+// f(streamed, lanes) of a kernel's template, as constants
+template <class F>
+static void with_lanes(bool s, int lanes, F &&f)
+{
+    if (lanes == 8) f(std::false_type{}, std::integral_constant<int, 8>{});
+    else if (lanes == 16) f(std::false_type{}, std::integral_constant<int, 16>{});
+    else if (lanes == 32) f(std::false_type{}, std::integral_constant<int, 32>{});
+    else if (s) f(std::true_type{}, std::integral_constant<int, 64>{});
+    else f(std::false_type{}, std::integral_constant<int, 64>{});
+}
+
+template <int DT>
+static hipError_t gather(const void *x, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out, hipStream_t st)
+{
+    const int lanes = lanes_of(cols, moe::per_piece(DT));
+    with_lanes(top_k == 1 && ld == cols && streams(x, x_rows, cols, DT), lanes, [&](auto s, auto g) {
+        moe_gather_kernel<DT, decltype(s)::value, decltype(g)::value><<<grid_of(rows, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
+                                                                                                            reinterpret_cast<uint8_t *>(out));
+    });
+    return hipGetLastError();
+}
+
+template <int DT, int OUT>
+static hipError_t combine(const void *y, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position, int64_t tokens, int32_t top_k, void *out, hipStream_t st)
+{
+    const int lanes = lanes_of(cols, DT == NVFP4_BF16 || OUT == NVFP4_BF16 ? 8 : 4);
+    with_lanes(streams(y, y_rows, cols, DT), lanes, [&](auto s, auto g) {
+        moe_combine_kernel<DT, OUT, decltype(s)::value, decltype(g)::value><<<grid_of(tokens, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position,
+                                                                                                                    tokens, top_k, reinterpret_cast<uint8_t *>(out));
+    });
+    return hipGetLastError();
+}
+
+template <int DT, int UP>
+static hipError_t combine_bwd(const void *dout, const void *y, int64_t rows, int64_t cols, const float *weights, const int32_t *position, const int32_t *kept, int64_t tokens,
+                              int32_t top_k, void *dy, float *dweights, hipStream_t st)
+{
+    const int64_t pairs = tokens * top_k, clearing = rows < 256 ? rows : 256;
+    const int lanes = lanes_of(cols, DT == NVFP4_BF16 || UP == NVFP4_BF16 ? 8 : 4);
+    with_lanes(streams(y, rows, cols, DT), lanes, [&](auto s, auto g) {
+        moe_combine_bwd_kernel<DT, UP, decltype(s)::value, decltype(g)::value><<<grid_of(pairs + clearing, lanes), 256, 0, st>>>(
+            reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols, weights, position, kept, pairs, top_k, reinterpret_cast<uint8_t *>(dy), dweights);
+    });
+    return hipGetLastError();
+}
 
 hipError_t launch_moe_gather(const void *x, int dt, int64_t x_rows, int64_t cols, int64_t ld, const int32_t *order, int32_t top_k, int64_t rows, void *out,
                              hipStream_t st)
 {
-    const bool s = top_k == 1 && ld == cols && streams(x, x_rows, cols, dt);
-    const int lanes = lanes_of(cols, dt);
-    auto *k = NVFP4_MOE_PICK(moe_gather_kernel, dt, s, lanes);
-    k<<<grid_of(rows, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(x), x_rows, cols, ld, order, top_k, rows,
-                                                       reinterpret_cast<uint8_t *>(out));
-    return hipGetLastError();
+    return dt == NVFP4_BF16 ? gather<NVFP4_BF16>(x, x_rows, cols, ld, order, top_k, rows, out, st) : gather<NVFP4_F32>(x, x_rows, cols, ld, order, top_k, rows, out, st);
 }
 
 hipError_t launch_moe_combine(const void *y, int dt, int64_t y_rows, int64_t cols, const float *weights, const int32_t *position, int64_t tokens,
-                              int32_t top_k, void *out, hipStream_t st)
+                              int32_t top_k, void *out, int out_dt, hipStream_t st)
 {
-    const bool s = streams(y, y_rows, cols, dt);
-    const int lanes = lanes_of(cols, dt);
-    auto *k = NVFP4_MOE_PICK(moe_combine_kernel, dt, s, lanes);
-    k<<<grid_of(tokens, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(y), y_rows, cols, weights, position, tokens, top_k,
-                                                         reinterpret_cast<uint8_t *>(out));
-    return hipGetLastError();
+    auto *f = dt == NVFP4_BF16 ? (out_dt == NVFP4_BF16 ? combine<NVFP4_BF16, NVFP4_BF16> : combine<NVFP4_BF16, NVFP4_F32>)
+                               : (out_dt == NVFP4_BF16 ? combine<NVFP4_F32, NVFP4_BF16> : combine<NVFP4_F32, NVFP4_F32>);
+    return f(y, y_rows, cols, weights, position, tokens, top_k, out, st);
 }
 
-hipError_t launch_moe_combine_bwd(const void *dout, const void *y, int dt, int64_t rows, int64_t cols, const float *weights, const int32_t *position,
+hipError_t launch_moe_combine_bwd(const void *dout, int dout_dt, const void *y, int dt, int64_t rows, int64_t cols, const float *weights, const int32_t *position,
                                   const int32_t *kept, int64_t tokens, int32_t top_k, void *dy, float *dweights, hipStream_t st)
 {
-    const int64_t pairs = tokens * top_k, clearing = rows < 256 ? rows : 256;
-    const bool s = streams(y, rows, cols, dt);
-    const int lanes = lanes_of(cols, dt);
-    auto *k = NVFP4_MOE_PICK(moe_combine_bwd_kernel, dt, s, lanes);
-    k<<<grid_of(pairs + clearing, lanes), 256, 0, st>>>(reinterpret_cast<const uint8_t *>(dout), reinterpret_cast<const uint8_t *>(y), rows, cols,
-                                                                   weights, position, kept, pairs, top_k, reinterpret_cast<uint8_t *>(dy), dweights);
-    return hipGetLastError();
+    auto *f = dt == NVFP4_BF16 ? (dout_dt == NVFP4_BF16 ? combine_bwd<NVFP4_BF16, NVFP4_BF16> : combine_bwd<NVFP4_BF16, NVFP4_F32>)
+                               : (dout_dt == NVFP4_BF16 ? combine_bwd<NVFP4_F32, NVFP4_BF16> : combine_bwd<NVFP4_F32, NVFP4_F32>);
+    return f(dout, y, rows, cols, weights, position, kept, tokens, top_k, dy, dweights, st);
 }
-
-#undef NVFP4_MOE_PICK
 
 }  // namespace nvfp4
