@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libnvfp4.so")
 
 RTN, SR = 0, 1
 F32, BF16 = 0, 1
+BF16_EXACT = 3  # of 8-bit products' results only
 SCALE_E4M3, SCALE_E8M0 = 0, 1
 PRESET_TSCALE = 1
 SLAB_ROWS = 2
@@ -784,8 +785,14 @@ def fp8_quantize(x: torch.Tensor, rows: bool = True, cols: bool = False, order: 
     return r, k
 
 
-def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
-    """nvfp4_fp8_gemm_ws: operands [M, K] and [N, K] -> [M, N]."""
+def _result_tag(out: torch.Tensor, exact: bool) -> int:
+    tag = _dtype_tag(out)
+    return BF16_EXACT if exact and tag == BF16 else tag
+
+
+def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, exact: bool = False) -> torch.Tensor:
+    """nvfp4_fp8_gemm_ws: operands [M, K] and [N, K] -> [M, N].  bf16 results come of the 8-bit instruction, which cuts small products off; with exact, of the
+    sums of binary32 results (here and in the experts' products)."""
     (M, K), (N, Kb) = a.codes.shape, b.codes.shape
     if K != Kb:
         raise ValueError(f"contractions of {K} and {Kb}")
@@ -796,7 +803,7 @@ def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch
         if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
             raise ValueError(f"out: [{M}, {N}] in rows of neighbouring elements")
         ldc = out.stride(0) if M > 1 else N
-    stream, tag = _stream(), _dtype_tag(out)
+    stream, tag = _stream(), _result_tag(out, exact)
     key = ("fp8_gemm", M, N, K, tag)
     ws_bytes = _known_sizes.get(key)
     if ws_bytes is None:
@@ -811,7 +818,7 @@ def fp8_gemm(a: Fp8, b: Fp8, out_dtype: torch.dtype = torch.bfloat16, out: torch
     return out
 
 
-def fp8_gemm_experts(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+def fp8_gemm_experts(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16, exact: bool = False) -> torch.Tensor:
     """nvfp4_fp8_gemm_experts: tokens in the experts' order [R, K] against their experts' rows of b [E * N, K] -> [R, N]."""
     (R, K), (EN, Kb), p_offsets, groups = a.codes.shape, b.codes.shape, _int32(offsets, "offsets"), offsets.numel() - 1
     if groups < 1 or EN % groups or Kb != K:
@@ -819,13 +826,13 @@ def fp8_gemm_experts(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dty
     N = EN // groups
     out = torch.empty(R, N, dtype=out_dtype, device=a.codes.device)
     code = lib.nvfp4_fp8_gemm_experts(R, N, K, groups, p_offsets, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(),
-                                      out.data_ptr(), _dtype_tag(out), N, _stream())
+                                      out.data_ptr(), _result_tag(out, exact), N, _stream())
     if code:
         _check(code, "nvfp4_fp8_gemm_experts")
     return out
 
 
-def fp8_gemm_experts_dw(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16, rows: int | None = None) -> torch.Tensor:
+def fp8_gemm_experts_dw(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.dtype = torch.bfloat16, rows: int | None = None, exact: bool = False) -> torch.Tensor:
     """nvfp4_fp8_gemm_experts_dw: columns operands [M, 128 S] and [N, 128 S] of two tensors with these offsets -> [E, M, N].
     rows: of these tensors (where left out, the most that S blocks can hold, which is as good)."""
     (M, width), (N, width_b), p_offsets, groups = a.codes.shape, b.codes.shape, _int32(offsets, "offsets"), offsets.numel() - 1
@@ -836,7 +843,7 @@ def fp8_gemm_experts_dw(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.
         raise ValueError(f"a, b: {rows // FP8_BLOCK + groups} blocks for {rows} rows of {groups} experts")
     out = torch.empty(groups, M, N, dtype=out_dtype, device=a.codes.device)
     _check(lib.nvfp4_fp8_gemm_experts_dw(M, N, rows, groups, p_offsets, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
-                                         b.scales.data_ptr(), out.data_ptr(), _dtype_tag(out), N, _stream()), "nvfp4_fp8_gemm_experts_dw")
+                                         b.scales.data_ptr(), out.data_ptr(), _result_tag(out, exact), N, _stream()), "nvfp4_fp8_gemm_experts_dw")
     return out
 
 

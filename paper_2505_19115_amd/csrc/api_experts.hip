@@ -21,8 +21,9 @@ inline int raw(const E &e)
     return v;
 }
 inline bool valid_dtype(int dt) { return dt == NVFP4_F32 || dt == NVFP4_BF16; }
+inline bool valid_result(int dt) { return valid_dtype(dt) || dt == NVFP4_BF16_EXACT; }
 inline bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-inline size_t elem(int dt) { return dt == NVFP4_BF16 ? 2 : 4; }
+inline size_t elem(int dt) { return out_bytes(dt); }
 inline nvfp4_status done(hipError_t e) { return e == hipSuccess ? NVFP4_OK : NVFP4_EHIP; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
 
@@ -81,7 +82,7 @@ nvfp4_status nvfp4_fp8_quantize(const void *x, nvfp4_dtype dt_, int64_t batch, i
 static nvfp4_status product(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32_t groups, const int32_t *offsets, int64_t total, const uint8_t *A_codes,
                             const uint8_t *A_scales, const uint8_t *B_codes, const uint8_t *B_scales, void *out, int out_dt, int64_t ldc, void *workspace, void *stream)
 {
-    if (!valid_dtype(out_dt)) return NVFP4_EINVAL;
+    if (!valid_result(out_dt)) return NVFP4_EINVAL;
     if (M < 0 || N < 0 || K < 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || ldc < N || M > MOST_ROWS || N > MOST_ROWS) return NVFP4_ESHAPE;
     if (mode != FP8_DENSE) {
         if (groups < 1 || groups > MAX_EXPERTS || !offsets) return NVFP4_EINVAL;
@@ -120,7 +121,7 @@ nvfp4_status nvfp4_fp8_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *A_co
 
 size_t nvfp4_fp8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, nvfp4_dtype out_dt)
 {
-    if (!valid_dtype(raw(out_dt)) || M <= 0 || N <= 0 || K <= 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || M > MOST_ROWS || N > MOST_ROWS) return 0;
+    if (!valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K <= 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || M > MOST_ROWS || N > MOST_ROWS) return 0;
     Fp8GemmArgs P = {};
     P.M = M;
     P.N = N;

@@ -79,6 +79,9 @@ struct Fp8GemmArgs {
     float *partial;                       // FP8_DIVIDED
     int32_t stream;                       // the output leaves by nontemporal stores (set by launch_fp8_gemm())
 };
+// Whether results of a type come of exact products in binary32 sums (fp8_gemm.h); their bytes
+constexpr bool exact_sums(int out_dt) { return out_dt != NVFP4_BF16; }
+constexpr int out_bytes(int out_dt) { return out_dt == NVFP4_F32 ? 4 : 2; }
 // The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
 // few tiles; 256 rows by 128 to 256 columns (binary32 outputs: 128); 128 x 128.
 double fp8_gemm_thin_cost(const Fp8GemmArgs &P);

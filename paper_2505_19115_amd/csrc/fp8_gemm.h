@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t four_scales(const uint8_t *scales, int64_t r
 //     off at 2^-13 of the power of two under its group's largest (the other 8-bit forms lose as much), and adds the groups in binary32: what is lost is at
 //     most 7 2^-13 = 8.5e-4 of sum |a||b|, reached only where single products stand far above the seven beside them, and 1.5e-5 of the result's norm for
 //     normal data, where rounding to bf16 takes 1.7e-3 of the norm.
-//   binary32 outputs: the codes become bf16, scale included (v_cvt_scalef32_pk_bf16_fp8), for v_mfma_f32_16x16x32_bf16, whose sums
+//   binary32 outputs, and bf16 ones of such sums (NVFP4_BF16_EXACT): the codes become bf16, scale included (v_cvt_scalef32_pk_bf16_fp8), for v_mfma_f32_16x16x32_bf16, whose sums
 //     are binary32 (1e-7 of the norm), at half the rate and for 32 conversions a lane.  That is exact for scale bytes LEAST .. MOST: below, the smallest codes
 //     need bits under bf16's least subnormal 2^-133, above, 448 * 2^(byte - 127) passes its largest number (a finite tensor's byte is 247 from
 //     1.75 * 2^127 on, torch.finfo(torch.bfloat16).min among them).  A wave that meets a block beyond these sums its outputs by multiply_codes().
@@ -240,6 +240,13 @@ __device__ __forceinline__ float4v_t multiply_codes(const Fp8GemmArgs &P, const 
         }
     }
     return acc;
+}
+
+template <int OUT_DT>
+__device__ __forceinline__ void store_one(void *out, int64_t at, float v)
+{
+    if (OUT_DT == NVFP4_F32) reinterpret_cast<float *>(out)[at] = v;
+    else reinterpret_cast<__bf16 *>(out)[at] = (__bf16)v;
 }
 
 // n of four columns of one row

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
         auto read = [&](const uint8_t *p, int j) -> Codes {
             return {*reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s0), *reinterpret_cast<const u32x4_t *>(p + 16 * j * KT + s1)};
         };
-        if constexpr (OUT_DT == NVFP4_F32) {
+        if constexpr (exact_sums(OUT_DT)) {
             // (blocks of the rows that there are)
             if (__builtin_expect(__ballot(far_bytes(sa, sb)) != 0, 0)) {
                 uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
         if (more) stash((kt + 1) & 1);
         __syncthreads();
     }
-    if (OUT_DT == NVFP4_F32 && __builtin_expect(__ballot(beyond) != 0, 0)) {
+    if (exact_sums(OUT_DT) && __builtin_expect(__ballot(beyond) != 0, 0)) {
 #pragma unroll 1
         for (int f = 0; f < 16; ++f) {
             const int r = ma + 4 * c + (f >> 2), s = nb + 4 * c + (f & 3);
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void fp8_gemm_kernel(Fp8GemmArgs P)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int col = wn * 64 + 16 * q + 4 * i + (f & 3);
-                if (row < T.rows && col < T.cols) reinterpret_cast<float *>(P.out)[(T.out + T.m0 + row) * P.ldc + T.n0 + col] = v[i];
+                if (row < T.rows && col < T.cols) store_one<OUT_DT>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col, v[i]);
             }
         }
         return;
@@ -155,7 +155,7 @@ template <int MODE>
 static hipError_t launch_tiles(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     constexpr int BM = 128, BN = 128, LDS = 2 * (BM + BN) * FP8_BLOCK;
-    auto *k = out_dt == NVFP4_F32 ? fp8_gemm_kernel<MODE, NVFP4_F32> : fp8_gemm_kernel<MODE, NVFP4_BF16>;
+    auto *k = out_dt == NVFP4_F32 ? fp8_gemm_kernel<MODE, NVFP4_F32> : out_dt == NVFP4_BF16 ? fp8_gemm_kernel<MODE, NVFP4_BF16> : fp8_gemm_kernel<MODE, NVFP4_BF16_EXACT>;
     k<<<launch_grid(f8g::tiles<MODE>(P, BM, BN)), 256, LDS, st>>>(P);
     return hipGetLastError();
 }
@@ -166,10 +166,10 @@ constexpr double K_TILE_BF16 = 0.95, K_TILE_F32 = 2.2;
 static double tiles_cost(int64_t tiles, int out_dt)
 {
     const int64_t slots = 2 * compute_units();
-    return (double)((tiles + slots - 1) / slots) * (out_dt == NVFP4_F32 ? K_TILE_F32 : K_TILE_BF16);
+    return (double)((tiles + slots - 1) / slots) * (exact_sums(out_dt) ? K_TILE_F32 : K_TILE_BF16);
 }
 // (expanding codes for binary32: 2000 x 2000 x 2000 44 / 34, 1056 x 2080 x 2784 36 / 43)
-static double thin_cost(const Fp8GemmArgs &P, int out_dt) { return fp8_gemm_thin_cost(P) * (out_dt == NVFP4_F32 ? 1.3 : 1.0); }
+static double thin_cost(const Fp8GemmArgs &P, int out_dt) { return fp8_gemm_thin_cost(P) * (exact_sums(out_dt) ? 1.3 : 1.0); }
 
 // Parts of the contraction of a dense product (1: not divided), where that is quicker than every kernel that does not divide it (3 and 2.5 us: their start) by more
 // than the host takes for the second launch: 16 x 64 x 12288 and 64 x 128 x 12288 would gain 1 us of 13 on the GPU alone.
@@ -200,13 +200,13 @@ static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
 {
     // Outputs past what the last cache level holds leave by streaming stores: 256 MB of weight gradients (8192 x 2 of 16, 4096 x 2048) 175 -> 155 us,
     // but 86 MB (4096 x 11008 x 4096) 154 -> 160, 128 MB the same.
-    P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * (out_dt == NVFP4_F32 ? 4 : 2) >= ((int64_t)256 << 20);
+    P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * out_bytes(out_dt) >= ((int64_t)256 << 20);
     const int64_t mine = f8g::tiles<MODE>(P, 128, 128), slots = 2 * compute_units();
     const double cost = tiles_cost(mine, out_dt);
     const double wide = P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE, out_dt) : 1e30;
     // An expert's few rows: 8 on average for bf16, 16 for binary32 (us, few rows / tiles: 64 tokens, 8 of 64, 1024 x 2048 38 / 40 and 39 / 68; 128 tokens 51 / 41 and
     // 51 / 68; 64 tokens, 2 of 8, 4096 x 4096 51 / 30 and 52 / 74)
-    if (MODE == FP8_EXPERTS && P.M <= (out_dt == NVFP4_BF16 ? 8 : 16) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
+    if (MODE == FP8_EXPERTS && P.M <= (exact_sums(out_dt) ? 16 : 8) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
     if (MODE == FP8_DENSE) {
         size_t bytes;
         const int parts = P.partial ? parts_of(P, out_dt, &bytes) : 1;

@@ -13,7 +13,7 @@ namespace nvfp4 {
 // MT, TN: fragments of 16 rows of A and of 16 columns.  U: K tiles of a batch (a wave without so many loads its last once more and does not multiply it).
 template <int MODE, int OUT_DT, int MT, int TN, int U, int NW>
 // (the experts' binary32 outputs: registers for as many waves a SIMD as hide the loads; 64 x 8 of 64 experts, 1024 x 2048, 37.6 us for 42.9 with one less)
-__global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32 ? (U == 4 ? 3 : U == 2 ? 4 : 5) : 1) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
+__global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && exact_sums(OUT_DT) ? (U == 4 ? 3 : U == 2 ? 4 : 5) : 1) void fp8_gemm_thin_kernel(Fp8GemmArgs P)
 {
     using namespace f8g;
     __shared__ float4v_t sums[NW][MT * TN][64];
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
     for (int a = 0; a < MT; ++a)
 #pragma unroll
         for (int b = 0; b < TN; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;  // (binary32 outputs) scale bytes
+    uint32_t least_a = ~0u, most_a = 0, least_b = ~0u, most_b = 0;  // (exact sums) scale bytes
     for (int kt = wave; kt < T.count; kt += NW * U) {
         Codes fb[U][TN], fa[U][MT];
         uint32_t sb[U][TN], sa[U][MT];
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (kt + u * NW < T.count) {
-                if constexpr (OUT_DT == NVFP4_F32) {
+                if constexpr (exact_sums(OUT_DT)) {
                     Expanded ea[MT];
 #pragma unroll
                     for (int a = 0; a < MT; ++a) ea[a] = expand(fa[u][a], sa[u][a]);
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
                 }
             }
         }
-        if constexpr (OUT_DT == NVFP4_F32) {
+        if constexpr (exact_sums(OUT_DT)) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
     }
     // blocks that bf16 does not hold, or of zeros: which, from memory (looked at above, codes would stay in registers longer)
     bool beyond = false;
-    if (OUT_DT == NVFP4_F32 && __builtin_expect(suspects(least_a, most_a, least_b, most_b), 0)) {
+    if (exact_sums(OUT_DT) && __builtin_expect(suspects(least_a, most_a, least_b, most_b), 0)) {
 #pragma unroll 1
         for (int f = 0; f < MT + TN; ++f) {
             const int r = 16 * (f < MT ? f : f - MT) + c;
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
             beyond |= any_beyond((f < MT ? P.A : P.B) + row * pitch + q * 16, (f < MT ? P.A_scales : P.B_scales) + row, f < MT ? P.a_rows : P.b_rows, wave, NW, T.count);
         }
     }
-    if (OUT_DT == NVFP4_F32 && __builtin_expect(__ballot(beyond) != 0, 0)) {
+    if (exact_sums(OUT_DT) && __builtin_expect(__ballot(beyond) != 0, 0)) {
 #pragma unroll 1
         for (int f = 0; f < MT * TN; ++f) {
             const int r = 16 * (f / TN) + c, s = 16 * (f % TN) + c;
@@ -135,7 +135,9 @@ __global__ __launch_bounds__(64 * NW, MODE == FP8_EXPERTS && OUT_DT == NVFP4_F32
 template <int MODE, int MT, int TN, int U, int NW>
 static hipError_t launch_batches(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
-    auto *k = out_dt == NVFP4_F32 ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, TN, U, NW> : fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, TN, U, NW>;
+    auto *k = out_dt == NVFP4_F32    ? fp8_gemm_thin_kernel<MODE, NVFP4_F32, MT, TN, U, NW>
+              : out_dt == NVFP4_BF16 ? fp8_gemm_thin_kernel<MODE, NVFP4_BF16, MT, TN, U, NW>
+                                     : fp8_gemm_thin_kernel<MODE, NVFP4_BF16_EXACT, MT, TN, U, NW>;
     k<<<launch_grid(f8g::tiles<MODE>(P, 16 * MT, 16 * TN)), 64 * NW, 0, st>>>(P);
     return hipGetLastError();
 }

@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
 #pragma unroll
             for (int b = 0; b < FB; ++b) acc[a][b] = float4v_t{0.0f, 0.0f, 0.0f, 0.0f};
         Codes A[8], B[FB];
-        bool beyond = false;  // (binary32 outputs) a block that bf16 does not hold
+        bool beyond = false;  // (exact sums) a block that bf16 does not hold
         auto read_a = [&](int st, int f, int h) { (h ? A[f].hi : A[f].lo) = *reinterpret_cast<const u32x4_t *>(baseA[st][h] + 16 * f * KT); };
         auto read_b = [&](int st, int f, int h) { (h ? B[f].hi : B[f].lo) = *reinterpret_cast<const u32x4_t *>(baseB[st][h] + 16 * f * KT); };
         // scales of fragments 4 i .. 4 i + 3 of the wave's part of A and of B, of tiles of either stage
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             if (kt + 2 >= T.count) past_end();
             asm volatile("s_nop 1");  // (accumulators that were just cleared: two instructions between that and the MFMAs)
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (OUT_DT == NVFP4_F32) {
+            if constexpr (exact_sums(OUT_DT)) {
                 // Halves as bf16: of A the one that is multiplied, of B both.  The compiler arranges what is between the barriers.
                 Expanded EA[4], EB[FB];
                 auto expand_a = [&](int h) {
@@ -490,7 +490,10 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                 float v[8];
                 // (reads that stay behind the wait states and leave the accumulators alone)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
+                for (int i = 0; i < 8; ++i) {
+                    if constexpr (exact_sums(OUT_DT)) v[i] = acc[a][2 * s + (i >> 2)][i & 3];
+                    else asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][2 * s + (i >> 2)][i & 3]));
+                }
                 return to_bf16(v) & keep;
             };
             constexpr int EACH = OUT_DT == NVFP4_F32 ? 16 : 32, N = 16 * FB / EACH;  // columns of such 64 bytes; how many
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
             NVFP4_F8W_WAIT(ALL + (decltype(inside)::value != 0 ? G::STORES : 0))
         };
         bool again = false;
-        if constexpr (OUT_DT == NVFP4_F32) again = keep != 0 && __ballot(beyond) != 0;  // (what no row holds may be anything)
+        if constexpr (exact_sums(OUT_DT)) again = keep != 0 && __ballot(beyond) != 0;  // (what no row holds may be anything)
         if (__builtin_expect(again, 0)) {
 #pragma unroll 1
             for (int f = 0; f < 8 * FB; ++f) {
@@ -534,8 +537,9 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                 const int64_t ra = T.m0 + (row < T.rows ? row : T.rows - 1), rb = T.b0 + T.n0 + (s < T.cols ? s : T.cols - 1);
                 const float4v_t v = multiply_codes(P, P.B + rb * pitch + q * 16, P.B_scales + rb, P.A + ra * pitch + q * 16, P.A_scales + ra, T.k0, 1, T.k0 + T.count);
                 if (DIVIDED) reinterpret_cast<float4v_t *>(P.partial)[(T.out * 4 + wave) * (8 * FB * 64) + f * 64 + lane] = v;
-                else if (row < T.rows && col < T.cols)
-                    store_lane<OUT_DT, false>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col, __builtin_bit_cast(u32x4_t, v) & keep, T.cols - col);
+                else
+                    for (int i = 0; i < 4; ++i)
+                        if (row < T.rows && col + i < T.cols) store_one<OUT_DT>(P.out, (T.out + T.m0 + row) * P.ldc + T.n0 + col + i, v[i]);
             }
             NVFP4_F8W_WAIT(ALL)
         } else if constexpr (DIVIDED) {
@@ -549,7 +553,7 @@ __global__ __launch_bounds__(256) void fp8_gemm_wide_kernel(Fp8GemmArgs P)
                     float4v_t v;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if constexpr (OUT_DT == NVFP4_F32) v[i] = acc[a][b][i];
+                        if constexpr (exact_sums(OUT_DT)) v[i] = acc[a][b][i];
                         else asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[i]) : "a"(acc[a][b][i]));
                     }
                     to[(a * FB + b) * 64] = v;
@@ -656,8 +660,8 @@ static int width_of(const Fp8GemmArgs &P, int mode, int out_dt, double *cost)
     const double k_tile[3] = {K_TILE_128, K_TILE_192, K_TILE_256};
     int best = 4;
     *cost = 1e30;
-    for (int fb = 4; fb <= (out_dt == NVFP4_F32 ? 4 : 8); fb += 2) {
-        const double c = (double)((rows * ((P.N + 32 * fb - 1) / (32 * fb)) + cus - 1) / cus) * (out_dt == NVFP4_F32 ? K_TILE_F32 : k_tile[fb / 2 - 2]);
+    for (int fb = 4; fb <= (exact_sums(out_dt) ? 4 : 8); fb += 2) {
+        const double c = (double)((rows * ((P.N + 32 * fb - 1) / (32 * fb)) + cus - 1) / cus) * (exact_sums(out_dt) ? K_TILE_F32 : k_tile[fb / 2 - 2]);
         if (c < *cost) {
             *cost = c;
             best = fb;
@@ -687,10 +691,10 @@ static int divided_width(const Fp8GemmArgs &P, int out_dt, int *parts, size_t *b
     *parts = 1;
     *bytes = 0;
     *cost = 1e30;
-    for (int fb = 4; fb <= (out_dt == NVFP4_F32 ? 4 : 8); fb += 2) {
+    for (int fb = 4; fb <= (exact_sums(out_dt) ? 4 : 8); fb += 2) {
         const int64_t tiles = rows * ((P.N + 32 * fb - 1) / (32 * fb));
         for (int n = 1; n <= MOST_PARTS && n * tiles <= cus && (n == 1 || n * PART <= P.blocks); ++n) {
-            const double c = (P.blocks + n - 1) / n * (out_dt == NVFP4_F32 ? K_TILE_F32 : k_tile[fb / 2 - 2]) + START +
+            const double c = (P.blocks + n - 1) / n * (exact_sums(out_dt) ? K_TILE_F32 : k_tile[fb / 2 - 2]) + START +
                              (n == 1 ? 0.0 : JOIN + 2.0 * n * (tiles / rows * 32 * fb) * ((P.M + 15) / 16 * 16) * 4 / JOIN_BYTES);
             if (c < *cost) {
                 *cost = c;
@@ -715,6 +719,7 @@ template <int MODE>
 static hipError_t launch_width(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
     if (out_dt == NVFP4_F32) return launch_wide<MODE, NVFP4_F32, 4>(P, st);
+    if (exact_sums(out_dt)) return launch_wide<MODE, NVFP4_BF16_EXACT, 4>(P, st);
     double cost;
     int parts;
     size_t bytes;
