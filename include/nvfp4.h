@@ -591,6 +591,12 @@ int nvfp4_host_layer_fused(int64_t M, int64_t N, int64_t K, nvfp4_dtype dt, cons
  * resident workgroups, the next tile in flight (flags as in those calls; rounding_rows counts for both = 1).  Not a promise. */
 int nvfp4_host_quantize_streams(int64_t rows, int64_t cols, int64_t ld, int both, int rounding_rows, int rounding_cols,
                                 const nvfp4_format *f, uint32_t flags);
+/* Which kernel serves an 8-bit product on the current device.  call: 0 nvfp4_fp8_gemm, 1 nvfp4_fp8_gemm_ws, 2 nvfp4_fp8_gemm_experts (M rows), 3
+ * nvfp4_fp8_gemm_experts_dw (K rows); groups of the last two; a dense output.  choice: 0 waves that divide the contraction (few rows), 1 tiles of 128 x
+ * 128, 2 of 256 rows, 3 of 256 rows with the contraction divided among workgroups; rows and columns of a workgroup's tile; K tiles that a wave loads at a
+ * time (of 0), workgroups of an output tile (of 3), else 1; whether the output leaves by streaming stores.  Returns 1, or 0 for sizes that launch nothing or
+ * are refused.  Not a promise: the rules follow measurements. */
+int nvfp4_host_fp8_gemm_kernel(int32_t call, int64_t M, int64_t N, int64_t K, int32_t groups, nvfp4_dtype out_dt, int32_t choice[5]);
 /* array forms: n inputs -> n outputs (host pointers) */
 void nvfp4_host_e4m3_encode_n(const float *r, int64_t n, uint8_t *out);
 void nvfp4_host_round_rtn_n(const float *m, int64_t n, uint8_t *out);

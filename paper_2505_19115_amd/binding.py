@@ -174,6 +174,8 @@ def _load() -> C.CDLL:
     L.nvfp4_fp8_gemm_ws.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, ci, i64, vp, sz, vp]
     L.nvfp4_fp8_gemm_experts.restype = L.nvfp4_fp8_gemm_experts_dw.restype = ci
     L.nvfp4_fp8_gemm_experts.argtypes = L.nvfp4_fp8_gemm_experts_dw.argtypes = [i64, i64, i64, i32, vp, vp, vp, vp, vp, vp, ci, i64, vp]
+    L.nvfp4_host_fp8_gemm_kernel.restype = ci
+    L.nvfp4_host_fp8_gemm_kernel.argtypes = [i32, i64, i64, i64, i32, ci, vp]
     L.nvfp4_moe_sort_workspace_bytes.argtypes = [i64, i32]
     L.nvfp4_moe_sort.restype = ci
     L.nvfp4_moe_sort.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, sz, vp]
@@ -224,7 +226,7 @@ EXPORTS = (
     "nvfp4_swiglu_bwd_workspace_bytes", "nvfp4_swiglu_bwd_quantize", "nvfp4_linear_bwd_dyq", "nvfp4_host_swiglu_bwd", "nvfp4_swiglu_bwd",
     "nvfp4_fp8_codes_bytes", "nvfp4_fp8_scales_bytes", "nvfp4_fp8_slots", "nvfp4_fp8_quantize", "nvfp4_fp8_gemm", "nvfp4_fp8_gemm_workspace_bytes", "nvfp4_fp8_gemm_ws", "nvfp4_fp8_gemm_experts",
     "nvfp4_fp8_gemm_experts_dw", "nvfp4_moe_sort_workspace_bytes", "nvfp4_moe_sort", "nvfp4_moe_gather", "nvfp4_moe_combine", "nvfp4_moe_combine_bwd",
-    "nvfp4_moe_combine_to", "nvfp4_moe_combine_to_bwd",
+    "nvfp4_moe_combine_to", "nvfp4_moe_combine_to_bwd", "nvfp4_host_fp8_gemm_kernel",
 )
 
 
@@ -845,6 +847,25 @@ def fp8_gemm_experts_dw(a: Fp8, b: Fp8, offsets: torch.Tensor, out_dtype: torch.
     _check(lib.nvfp4_fp8_gemm_experts_dw(M, N, rows, groups, p_offsets, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(),
                                          b.scales.data_ptr(), out.data_ptr(), _result_tag(out, exact), N, _stream()), "nvfp4_fp8_gemm_experts_dw")
     return out
+
+
+class Fp8Kernel(NamedTuple):
+    """What serves a product: "few rows", "tiles", "wide" or "divided"; rows and columns of a workgroup's tile; K tiles of a wave's batch (few rows) or workgroups
+    of a tile (divided), else 1; whether the output is streamed."""
+    name: str
+    rows: int
+    cols: int
+    parts: int
+    streamed: bool
+
+
+def fp8_gemm_kernel(call: str, M: int, N: int, K: int, groups: int = 0, out_dtype: torch.dtype = torch.bfloat16, exact: bool = False) -> Fp8Kernel | None:
+    """nvfp4_host_fp8_gemm_kernel of a call: "nvfp4_fp8_gemm", "fp8_gemm", "fp8_gemm_experts" (M rows) or "fp8_gemm_experts_dw" (K rows).  None: no kernel."""
+    which = ("nvfp4_fp8_gemm", "fp8_gemm", "fp8_gemm_experts", "fp8_gemm_experts_dw").index(call)
+    choice = (C.c_int32 * 5)()
+    if not lib.nvfp4_host_fp8_gemm_kernel(which, M, N, K, groups, F32 if out_dtype is torch.float32 else BF16_EXACT if exact else BF16, choice):
+        return None
+    return Fp8Kernel(("few rows", "tiles", "wide", "divided")[choice[0]], choice[1], choice[2], choice[3], bool(choice[4]))
 
 
 def moe_sort(experts: torch.Tensor, groups: int) -> MoeOrder:

@@ -156,6 +156,28 @@ nvfp4_status nvfp4_fp8_gemm_experts_dw(int64_t M, int64_t N, int64_t rows, int32
                    nullptr, stream);
 }
 
+int nvfp4_host_fp8_gemm_kernel(int32_t call, int64_t M, int64_t N, int64_t K, int32_t groups, nvfp4_dtype out_dt, int32_t choice[5])
+{
+    const Fp8Mode mode = call == 2 ? FP8_EXPERTS : call == 3 ? FP8_EXPERTS_DW : FP8_DENSE;
+    if (call < 0 || call > 3 || !choice || !valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K < 0 || M > MOST_ROWS || N > MOST_ROWS || K > MOST_ROWS) return 0;
+    if (mode != FP8_DENSE && (groups < 1 || groups > MAX_EXPERTS)) return 0;
+    if (mode == FP8_EXPERTS_DW) K = FP8_BLOCK * fp8_slots(K, groups);
+    if (K % FP8_BLOCK != 0 || K > MOST_WIDTH) return 0;
+    Fp8GemmArgs P = {};
+    P.M = M;
+    P.N = N;
+    P.ldc = N;
+    P.blocks = (int32_t)(K / FP8_BLOCK);
+    P.groups = mode == FP8_DENSE ? 0 : groups;
+    const Fp8Choice c = fp8_gemm_choice(P, mode, raw(out_dt), call == 1);
+    choice[0] = c.kernel;
+    choice[1] = c.rows;
+    choice[2] = c.cols;
+    choice[3] = c.parts;
+    choice[4] = c.stream;
+    return 1;
+}
+
 size_t nvfp4_moe_sort_workspace_bytes(int64_t pairs, int32_t groups)
 {
     return pairs > 0 && pairs <= MOST_ROWS && groups >= 1 && groups <= MAX_EXPERTS ? moe_sort_workspace(pairs, groups) : 0;

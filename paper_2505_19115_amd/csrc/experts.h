@@ -82,12 +82,22 @@ struct Fp8GemmArgs {
 // Whether results of a type come of exact products in binary32 sums (fp8_gemm.h); their bytes
 constexpr bool exact_sums(int out_dt) { return out_dt != NVFP4_BF16; }
 constexpr int out_bytes(int out_dt) { return out_dt == NVFP4_F32 ? 4 : 2; }
+// Which kernel, the rows and columns of a workgroup's tile, K tiles of a batch (few rows) or workgroups of a tile (divided), else 1, and whether the output is streamed
+struct Fp8Choice {
+    enum Kernel { FEW_ROWS, TILES, WIDE, DIVIDED } kernel;
+    int rows, cols, parts;
+    bool stream;
+};
+// `scratch`: of a dense product, whether there is memory at `partial`
+Fp8Choice fp8_gemm_choice(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, bool scratch);
 // The kernels that launch_fp8_gemm() chooses from, with what a K tile of the contraction takes them, in us: waves that divide the contraction, for outputs of
 // few tiles; 256 rows by 128 to 256 columns (binary32 outputs: 128); 128 x 128.
 double fp8_gemm_thin_cost(const Fp8GemmArgs &P);
-hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
+void fp8_gemm_thin_choice(const Fp8GemmArgs &P, Fp8Mode mode, Fp8Choice *c);
+hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, const Fp8Choice &c, hipStream_t st);
 double fp8_gemm_wide_cost(const Fp8GemmArgs &P, int mode, int out_dt);
-hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st);
+int fp8_gemm_wide_cols(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt);  // of a tile
+hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, int cols, hipStream_t st);
 int64_t compute_units();
 // Among how many workgroups that kernel divides a dense product's contraction to be quickest (1: not at all, or not in less than `below` us), the bytes that it then
 // needs at `partial`, and its time in us

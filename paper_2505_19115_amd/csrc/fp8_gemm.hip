@@ -196,37 +196,63 @@ size_t fp8_gemm_workspace(const Fp8GemmArgs &P, int out_dt)
 }
 
 template <int MODE>
-static hipError_t launch(Fp8GemmArgs P, int out_dt, hipStream_t st)
+static Fp8Choice choose(const Fp8GemmArgs &P, int out_dt, bool scratch)
 {
+    Fp8Choice c{Fp8Choice::TILES, 128, 128, 1, false};
     // Outputs past what the last cache level holds leave by streaming stores: 256 MB of weight gradients (8192 x 2 of 16, 4096 x 2048) 175 -> 155 us,
     // but 86 MB (4096 x 11008 x 4096) 154 -> 160, 128 MB the same.
-    P.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * out_bytes(out_dt) >= ((int64_t)256 << 20);
+    c.stream = (MODE == FP8_EXPERTS_DW ? P.groups : 1) * P.M * P.ldc * out_bytes(out_dt) >= ((int64_t)256 << 20);
     const int64_t mine = f8g::tiles<MODE>(P, 128, 128), slots = 2 * compute_units();
     const double cost = tiles_cost(mine, out_dt);
     const double wide = P.blocks > 0 ? fp8_gemm_wide_cost(P, MODE, out_dt) : 1e30;
+    auto few_rows = [&]() {
+        c.kernel = Fp8Choice::FEW_ROWS;
+        fp8_gemm_thin_choice(P, (Fp8Mode)MODE, &c);
+        return c;
+    };
     // An expert's few rows: 8 on average for bf16, 16 for binary32 (us, few rows / tiles: 64 tokens, 8 of 64, 1024 x 2048 38 / 40 and 39 / 68; 128 tokens 51 / 41 and
     // 51 / 68; 64 tokens, 2 of 8, 4096 x 4096 51 / 30 and 52 / 74)
-    if (MODE == FP8_EXPERTS && P.M <= (exact_sums(out_dt) ? 16 : 8) * (int64_t)P.groups) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
+    if (MODE == FP8_EXPERTS && P.M <= (exact_sums(out_dt) ? 16 : 8) * (int64_t)P.groups) return few_rows();
     if (MODE == FP8_DENSE) {
         size_t bytes;
-        const int parts = P.partial ? parts_of(P, out_dt, &bytes) : 1;
-        if (parts > 1) {
-            P.groups = parts;
-            return launch_fp8_gemm_wide(P, FP8_DIVIDED, out_dt, st);
+        c.parts = scratch ? parts_of(P, out_dt, &bytes) : 1;
+        if (c.parts > 1) {
+            c.kernel = Fp8Choice::DIVIDED;
+            c.rows = 256;
+            c.cols = fp8_gemm_wide_cols(P, FP8_DIVIDED, out_dt);
+            return c;
         }
         const double thin = thin_cost(P, out_dt);
-        if (thin < cost && thin < wide) return launch_fp8_gemm_thin(P, (Fp8Mode)MODE, out_dt, st);
+        if (thin < cost && thin < wide) return few_rows();
     }
     // A short contraction in few tiles: the larger ones take 1 to 2 us more to begin and end (experts 300 tokens, 3 of 10, 500 x 700 8.7 / 10.5, their weight
     // gradients 7.1 / 8.5)
     const int32_t count = MODE == FP8_EXPERTS_DW ? P.blocks / P.groups : P.blocks;
-    if (wide < cost && !(count <= 6 && mine <= slots / 2)) return launch_fp8_gemm_wide(P, (Fp8Mode)MODE, out_dt, st);
-    return launch_tiles<MODE>(P, out_dt, st);
+    if (wide < cost && !(count <= 6 && mine <= slots / 2)) {
+        c.kernel = Fp8Choice::WIDE;
+        c.rows = 256;
+        c.cols = fp8_gemm_wide_cols(P, (Fp8Mode)MODE, out_dt);
+    }
+    return c;
 }
 
-hipError_t launch_fp8_gemm(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
+Fp8Choice fp8_gemm_choice(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, bool scratch)
 {
-    return mode == FP8_DENSE ? launch<FP8_DENSE>(P, out_dt, st) : mode == FP8_EXPERTS ? launch<FP8_EXPERTS>(P, out_dt, st) : launch<FP8_EXPERTS_DW>(P, out_dt, st);
+    return mode == FP8_DENSE ? choose<FP8_DENSE>(P, out_dt, scratch) : mode == FP8_EXPERTS ? choose<FP8_EXPERTS>(P, out_dt, scratch) : choose<FP8_EXPERTS_DW>(P, out_dt, scratch);
+}
+
+hipError_t launch_fp8_gemm(const Fp8GemmArgs &args, Fp8Mode mode, int out_dt, hipStream_t st)
+{
+    Fp8GemmArgs P = args;
+    const Fp8Choice c = fp8_gemm_choice(P, mode, out_dt, P.partial != nullptr);
+    P.stream = c.stream;
+    if (c.kernel == Fp8Choice::FEW_ROWS) return launch_fp8_gemm_thin(P, mode, out_dt, c, st);
+    if (c.kernel == Fp8Choice::WIDE) return launch_fp8_gemm_wide(P, mode, out_dt, c.cols, st);
+    if (c.kernel == Fp8Choice::DIVIDED) {
+        P.groups = c.parts;
+        return launch_fp8_gemm_wide(P, FP8_DIVIDED, out_dt, c.cols, st);
+    }
+    return mode == FP8_DENSE ? launch_tiles<FP8_DENSE>(P, out_dt, st) : mode == FP8_EXPERTS ? launch_tiles<FP8_EXPERTS>(P, out_dt, st) : launch_tiles<FP8_EXPERTS_DW>(P, out_dt, st);
 }
 
 }  // namespace nvfp4

@@ -143,21 +143,26 @@ static hipError_t launch_batches(const Fp8GemmArgs &P, int out_dt, hipStream_t s
 }
 
 // (batches of no more K tiles than a wave has: 64 experts of 1024 x 2048 with 2 tokens each, 16 K tiles, 64 us in batches of 4 by 8 waves, 30 by 4)
+static int batch_of(const Fp8GemmArgs &P, int most, int waves) { return most >= 4 && P.blocks >= 4 * waves ? 4 : most >= 2 && P.blocks >= 2 * waves ? 2 : 1; }
 template <int MODE, int MT, int TN, int U, int NW>
 static hipError_t launch_thin(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
 {
-    if (U >= 4 && P.blocks >= 4 * NW) return launch_batches<MODE, MT, TN, U, NW>(P, out_dt, st);
-    if (U >= 2 && P.blocks >= 2 * NW) return launch_batches<MODE, MT, TN, U < 2 ? U : 2, NW>(P, out_dt, st);
+    const int batch = batch_of(P, U, NW);
+    if (batch == 4) return launch_batches<MODE, MT, TN, U < 4 ? U : 4, NW>(P, out_dt, st);
+    if (batch == 2) return launch_batches<MODE, MT, TN, U < 2 ? U : 2, NW>(P, out_dt, st);
     return launch_batches<MODE, MT, TN, 1, NW>(P, out_dt, st);
 }
 
-// Shapes of a workgroup's output: rows and columns in 16s.  What bounds these kernels is what a CU's loads bring, (MT + TN) * 16 rows of a K tile at 36 GB/s: the
-// fewest rounds of the CUs times that.  us, 16 rows, 48 columns at most / 64: 16384 x 4096 18.3 / 15.5, 28672 x 4096 32.5 / 28.3, 12288 x 4096 13.0 / 12.1.
+// Shapes of a workgroup's output, rows and columns in 16s, and its largest batch.  What bounds these kernels is what a CU's loads bring, (MT + TN) * 16 rows of a K tile at
+// 36 GB/s: the fewest rounds of the CUs times that.  us, 16 rows, 48 columns at most / 64: 16384 x 4096 18.3 / 15.5, 28672 x 4096 32.5 / 28.3, 12288 x 4096 13.0 / 12.1.
 namespace f8t {
 struct Shape {
-    int mt, tn;
+    int mt, tn, u;
 };
-constexpr Shape SHAPES[] = {{1, 1}, {1, 2}, {1, 3}, {1, 4}, {2, 1}, {2, 2}, {2, 3}, {2, 4}, {4, 2}, {4, 3}, {4, 4}};
+constexpr Shape SHAPES[] = {{1, 1, 4}, {1, 2, 4}, {1, 3, 4}, {1, 4, 4}, {2, 1, 4}, {2, 2, 2}, {2, 3, 2}, {2, 4, 2}, {4, 2, 2}, {4, 3, 1}, {4, 4, 1}};
+constexpr int N_SHAPES = sizeof(SHAPES) / sizeof(SHAPES[0]), WAVES = 8;
+constexpr Shape EXPERTS = {1, 2, 4};
+constexpr int EXPERTS_WAVES = 4;
 constexpr double PER_16_ROWS = 0.057;  // us
 
 inline int64_t workgroups(const Fp8GemmArgs &P, Shape s)
@@ -166,16 +171,17 @@ inline int64_t workgroups(const Fp8GemmArgs &P, Shape s)
 }
 }  // namespace f8t
 
-static f8t::Shape shape_of(const Fp8GemmArgs &P, double *cost)
+static int shape_of(const Fp8GemmArgs &P, double *cost)
 {
     const int64_t cus = compute_units();
-    f8t::Shape best = f8t::SHAPES[0];
+    int best = 0;
     *cost = 1e30;
-    for (const f8t::Shape s : f8t::SHAPES) {
+    for (int i = 0; i < f8t::N_SHAPES; ++i) {
+        const f8t::Shape s = f8t::SHAPES[i];
         const double c = (double)((f8t::workgroups(P, s) + cus - 1) / cus) * (s.mt + s.tn) * f8t::PER_16_ROWS;
         if (c < *cost) {
             *cost = c;
-            best = s;
+            best = i;
         }
     }
     return best;
@@ -188,24 +194,28 @@ double fp8_gemm_thin_cost(const Fp8GemmArgs &P)
     return cost;
 }
 
-hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
+void fp8_gemm_thin_choice(const Fp8GemmArgs &P, Fp8Mode mode, Fp8Choice *c)
 {
-    if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, 1, 2, 4, 4>(P, out_dt, st);
     double cost;
-    const f8t::Shape s = shape_of(P, &cost);
-    switch (4 * s.mt + s.tn) {
-    case 5: return launch_thin<FP8_DENSE, 1, 1, 4, 8>(P, out_dt, st);
-    case 6: return launch_thin<FP8_DENSE, 1, 2, 4, 8>(P, out_dt, st);
-    case 7: return launch_thin<FP8_DENSE, 1, 3, 4, 8>(P, out_dt, st);
-    case 8: return launch_thin<FP8_DENSE, 1, 4, 4, 8>(P, out_dt, st);
-    case 9: return launch_thin<FP8_DENSE, 2, 1, 4, 8>(P, out_dt, st);
-    case 10: return launch_thin<FP8_DENSE, 2, 2, 2, 8>(P, out_dt, st);
-    case 11: return launch_thin<FP8_DENSE, 2, 3, 2, 8>(P, out_dt, st);
-    case 12: return launch_thin<FP8_DENSE, 2, 4, 2, 8>(P, out_dt, st);
-    case 18: return launch_thin<FP8_DENSE, 4, 2, 2, 8>(P, out_dt, st);
-    case 19: return launch_thin<FP8_DENSE, 4, 3, 1, 8>(P, out_dt, st);
-    default: return launch_thin<FP8_DENSE, 4, 4, 1, 8>(P, out_dt, st);
-    }
+    const f8t::Shape s = mode == FP8_EXPERTS ? f8t::EXPERTS : f8t::SHAPES[shape_of(P, &cost)];
+    c->rows = 16 * s.mt;
+    c->cols = 16 * s.tn;
+    c->parts = batch_of(P, s.u, mode == FP8_EXPERTS ? f8t::EXPERTS_WAVES : f8t::WAVES);
+}
+
+template <int I>
+static hipError_t launch_shape(const Fp8Choice &c, const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+{
+    constexpr f8t::Shape S = f8t::SHAPES[I];
+    if (c.rows == 16 * S.mt && c.cols == 16 * S.tn) return launch_thin<FP8_DENSE, S.mt, S.tn, S.u, f8t::WAVES>(P, out_dt, st);
+    if constexpr (I + 1 < f8t::N_SHAPES) return launch_shape<I + 1>(c, P, out_dt, st);
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_fp8_gemm_thin(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, const Fp8Choice &c, hipStream_t st)
+{
+    if (mode == FP8_EXPERTS) return launch_thin<FP8_EXPERTS, f8t::EXPERTS.mt, f8t::EXPERTS.tn, f8t::EXPERTS.u, f8t::EXPERTS_WAVES>(P, out_dt, st);
+    return launch_shape<0>(c, P, out_dt, st);
 }
 
 }  // namespace nvfp4

@@ -715,22 +715,27 @@ int fp8_gemm_parts(const Fp8GemmArgs &P, int out_dt, double below, size_t *bytes
     return parts;
 }
 
-template <int MODE>
-static hipError_t launch_width(const Fp8GemmArgs &P, int out_dt, hipStream_t st)
+int fp8_gemm_wide_cols(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt)
 {
-    if (out_dt == NVFP4_F32) return launch_wide<MODE, NVFP4_F32, 4>(P, st);
-    if (exact_sums(out_dt)) return launch_wide<MODE, NVFP4_BF16_EXACT, 4>(P, st);
     double cost;
     int parts;
     size_t bytes;
-    const int fb = MODE == FP8_DIVIDED ? divided_width(P, out_dt, &parts, &bytes, &cost) : width_of(P, MODE, out_dt, &cost);
-    return fb == 4 ? launch_wide<MODE, NVFP4_BF16, 4>(P, st) : fb == 6 ? launch_wide<MODE, NVFP4_BF16, 6>(P, st) : launch_wide<MODE, NVFP4_BF16, 8>(P, st);
+    return 32 * (mode == FP8_DIVIDED ? divided_width(P, out_dt, &parts, &bytes, &cost) : width_of(P, mode, out_dt, &cost));
 }
 
-hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, hipStream_t st)
+template <int MODE>
+static hipError_t launch_width(const Fp8GemmArgs &P, int out_dt, int cols, hipStream_t st)
 {
-    if (mode == FP8_DIVIDED) return launch_width<FP8_DIVIDED>(P, out_dt, st);
-    return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, out_dt, st) : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, out_dt, st) : launch_width<FP8_EXPERTS_DW>(P, out_dt, st);
+    if (out_dt == NVFP4_F32) return launch_wide<MODE, NVFP4_F32, 4>(P, st);
+    if (exact_sums(out_dt)) return launch_wide<MODE, NVFP4_BF16_EXACT, 4>(P, st);
+    return cols == 128 ? launch_wide<MODE, NVFP4_BF16, 4>(P, st) : cols == 192 ? launch_wide<MODE, NVFP4_BF16, 6>(P, st) : launch_wide<MODE, NVFP4_BF16, 8>(P, st);
+}
+
+hipError_t launch_fp8_gemm_wide(const Fp8GemmArgs &P, Fp8Mode mode, int out_dt, int cols, hipStream_t st)
+{
+    if (mode == FP8_DIVIDED) return launch_width<FP8_DIVIDED>(P, out_dt, cols, st);
+    return mode == FP8_DENSE ? launch_width<FP8_DENSE>(P, out_dt, cols, st)
+           : mode == FP8_EXPERTS ? launch_width<FP8_EXPERTS>(P, out_dt, cols, st) : launch_width<FP8_EXPERTS_DW>(P, out_dt, cols, st);
 }
 
 }  // namespace nvfp4
