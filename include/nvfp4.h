@@ -432,6 +432,8 @@ nvfp4_status nvfp4_quant_noise(const void *x, nvfp4_dtype dt, int64_t rows, int6
  *   scales  [S, rows] bytes, E8M0 (2^(byte - 127)): block-major, the bytes of neighbouring rows side by side.
  * Pointers and pitches of tensors (x, out, y, ...) need the alignment of an element only; codes must be 16-byte aligned.
  * Empty tensors (a size of 0) are accepted where said; their pointers may be NULL.
+ * Sizes past these limits are refused (NVFP4_ESHAPE): 2^31 - 1 rows of an operand (batch * rows, groups * N) and of an
+ * output, contractions and widths to quantize of 2^23 (a columns side contracts its rows), outputs of 2^31 - 1 tiles of 16 x 16.
  */
 size_t nvfp4_fp8_codes_bytes(int64_t rows, int64_t K);
 size_t nvfp4_fp8_scales_bytes(int64_t rows, int64_t K);
