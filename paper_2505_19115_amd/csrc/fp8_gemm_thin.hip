@@ -3,8 +3,8 @@
 // every lane loads its own codes, 32 of a row and K tile, a batch of K tiles at a time.  The waves' sums are added through the LDS
 // in the waves' order.
 //
-// What bounds it: loads in flight, and the first of them, which an expert's product asks for behind its offsets.  16 x 11008 x 4096 11.4 us, 4.0 TB/s; 16 x 16384 x
-// 4096 15.5 us, 4.4 TB/s; 8 experts of 2048 x 4096, 16 rows 17.3 us, 3.9 TB/s; a token's 2 of them 7.0 us, where one 4096 x 4096 takes 5.1.  Without effect: lanes that load
+// What bounds it: loads in flight, and the first of them, which an expert's product asks for behind its offsets.  16 x 11008 x 4096 11.6 us, 3.9 TB/s; 16 x 16384 x
+// 4096 15.7 us, 4.3 TB/s; 8 experts of 2048 x 4096, 16 rows 18.7 us, 3.6 TB/s (10.5, 12.8 and 17 where the last cache level has the weights); a token's 2 of them 7.0 us, where one 4096 x 4096 takes 5.1.  Without effect: lanes that load
 // whole lines; slower: streaming loads (16 x 11008 x 4096 12.8 us), the experts' products on more columns (20 us) or more waves (20 us).
 #include "fp8_gemm.h"
 

@@ -4,9 +4,10 @@
 // with an infinity or a NaN becomes NaN codes, so that the product shows it.  The scale is a power of two because that is what the
 // matrix instruction applies by itself: a product with binary32 scales would need a multiply-add per output and 128 elements.
 //
-// What bounds it is memory: 2 or 4 bytes per element in, 1 out (2 where both sides are wanted, from one read).  bf16 4096 x 11008, rows 24.6 us (5.5
-// TB/s, what a copy reaches), both sides 38.3 (4.7 TB/s: the columns' codes leave in pieces of 128 bytes, a column pitch apart); 16 matrices 4096 x 2048 both sides
-// 95 (5.7); 8192 x 2048 gathered to 16384 rows, both sides by expert 36 (3.7 TB/s with the rows read twice); 16 x 4096 3.1, latency.
+// What bounds it is memory: 2 or 4 bytes per element in, 1 out (2 where both sides are wanted, from one read).  bf16 4096 x 11008, rows 24.2 us (5.6
+// TB/s, what a copy reaches), both sides 35 (5.2) where the last cache level still has the tensor, 37 to 42 (4.3 to 4.8) from memory: the columns' codes leave in pieces of 128
+// bytes, a column pitch apart; 16 matrices 4096 x 2048 both sides 91 (5.9); 8192 x 2048 gathered to 16384 rows, both sides by expert 32 to 36 (3.7 to 4.2 TB/s with the rows
+// read twice); 16 x 4096 3.0, latency.
 #include "experts.h"
 
 namespace nvfp4 {

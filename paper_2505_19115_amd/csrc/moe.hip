@@ -6,8 +6,8 @@
 //   combine       out[t] = sum_j w[t, j] y[position[t, j]], choices in their order, binary32
 //   combine_bwd   dy[position[t, j]] = w[t, j] dout[t],  dw[t, j] = sum_d dout[t, d] y[position[t, j], d]
 // What bounds rows is memory, at what a copy reaches (5.3 TB/s): a wave moves a row (of a pair, or of a token with its choices) in pieces of 16 bytes a lane.
-// 8192 tokens x 2 of 4096 bf16, combined 39.6 us (5.1 TB/s), gradient 52 to 62 (5.4 to 6.4, by what the last cache level still holds); 1777 x 4 of 1027 binary32
-// gathered 9.7 (3.8 TB/s: rows that share lines).  The sort is bound by latency: 32 pairs of 8 experts 3.3 us in one workgroup, 262144 of 128 experts 3.2 + 9.3
+// 8192 tokens x 2 of 4096 bf16, combined 38 to 41 us (4.9 to 5.3 TB/s), binary32 rows into bf16 70 (4.8), gradient 52 to 64 (5.2 to 6.4, by what the last cache level still
+// holds); 1777 x 4 of 1027 binary32 gathered 9.7 (3.8 TB/s: rows that share lines; 10.8 from memory).  The sort is bound by latency: 32 pairs of 8 experts 3.3 us in one workgroup, 262144 of 128 experts 3.2 + 9.3
 // in 64 of them (128 and 256 the same), where its 4 MB take 0.8.
 #include <type_traits>
 
