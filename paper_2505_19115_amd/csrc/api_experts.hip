@@ -79,16 +79,21 @@ nvfp4_status nvfp4_fp8_quantize(const void *x, nvfp4_dtype dt_, int64_t batch, i
     return done(launch_fp8_quantize(P, dt, reinterpret_cast<hipStream_t>(stream)));
 }
 
+// Sizes of a product: within what the operands, offsets and launches count
+static bool valid_sizes(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32_t groups)
+{
+    if (M < 0 || N < 0 || K < 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || M > MOST_ROWS || N > MOST_ROWS) return false;
+    if (mode != FP8_DENSE && (mode == FP8_EXPERTS ? groups * N : groups * M) > MOST_ROWS) return false;
+    return (ceil_div(M, 16) + groups + 1) * ceil_div(N, 16) <= MOST_GRID / (mode == FP8_EXPERTS_DW ? groups : 1);
+}
+
 static nvfp4_status product(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32_t groups, const int32_t *offsets, int64_t total, const uint8_t *A_codes,
                             const uint8_t *A_scales, const uint8_t *B_codes, const uint8_t *B_scales, void *out, int out_dt, int64_t ldc, void *workspace, void *stream)
 {
     if (!valid_result(out_dt)) return NVFP4_EINVAL;
-    if (M < 0 || N < 0 || K < 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || ldc < N || M > MOST_ROWS || N > MOST_ROWS) return NVFP4_ESHAPE;
-    if (mode != FP8_DENSE) {
-        if (groups < 1 || groups > MAX_EXPERTS || !offsets) return NVFP4_EINVAL;
-        if (mode == FP8_EXPERTS ? groups * N > MOST_ROWS : groups * M > MOST_ROWS) return NVFP4_ESHAPE;
-        if (!aligned(offsets, 4)) return NVFP4_EALIGN;
-    }
+    if (mode != FP8_DENSE && (groups < 1 || groups > MAX_EXPERTS || !offsets)) return NVFP4_EINVAL;
+    if (ldc < N || !valid_sizes(mode, M, N, K, groups)) return NVFP4_ESHAPE;
+    if (mode != FP8_DENSE && !aligned(offsets, 4)) return NVFP4_EALIGN;
     if (M == 0 || N == 0) return NVFP4_OK;
     const nvfp4_status s = check_product(A_codes, A_scales, B_codes, B_scales, out, out_dt, K > 0);
     if (s != NVFP4_OK) return s;
@@ -108,7 +113,6 @@ static nvfp4_status product(Fp8Mode mode, int64_t M, int64_t N, int64_t K, int32
     P.groups = mode == FP8_DENSE ? 0 : groups;
     P.total = (int32_t)total;
     P.partial = reinterpret_cast<float *>(workspace);
-    if ((ceil_div(M, 16) + groups + 1) * ceil_div(N, 16) > MOST_GRID / (mode == FP8_EXPERTS_DW ? groups : 1)) return NVFP4_ESHAPE;
     return done(launch_fp8_gemm(P, mode, out_dt, reinterpret_cast<hipStream_t>(stream)));
 }
 
@@ -121,7 +125,7 @@ nvfp4_status nvfp4_fp8_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *A_co
 
 size_t nvfp4_fp8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, nvfp4_dtype out_dt)
 {
-    if (!valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K <= 0 || K % FP8_BLOCK != 0 || K > MOST_WIDTH || M > MOST_ROWS || N > MOST_ROWS) return 0;
+    if (!valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K <= 0 || !valid_sizes(FP8_DENSE, M, N, K, 0)) return 0;
     Fp8GemmArgs P = {};
     P.M = M;
     P.N = N;
@@ -159,16 +163,17 @@ nvfp4_status nvfp4_fp8_gemm_experts_dw(int64_t M, int64_t N, int64_t rows, int32
 int nvfp4_host_fp8_gemm_kernel(int32_t call, int64_t M, int64_t N, int64_t K, int32_t groups, nvfp4_dtype out_dt, int32_t choice[5])
 {
     const Fp8Mode mode = call == 2 ? FP8_EXPERTS : call == 3 ? FP8_EXPERTS_DW : FP8_DENSE;
-    if (call < 0 || call > 3 || !choice || !valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K < 0 || M > MOST_ROWS || N > MOST_ROWS || K > MOST_ROWS) return 0;
-    if (mode != FP8_DENSE && (groups < 1 || groups > MAX_EXPERTS)) return 0;
+    if (call < 0 || call > 3 || !choice || !valid_result(raw(out_dt)) || M <= 0 || N <= 0 || K < 0 || K > MOST_ROWS) return 0;
+    if (mode == FP8_DENSE) groups = 0;
+    else if (groups < 1 || groups > MAX_EXPERTS) return 0;
     if (mode == FP8_EXPERTS_DW) K = FP8_BLOCK * fp8_slots(K, groups);
-    if (K % FP8_BLOCK != 0 || K > MOST_WIDTH) return 0;
+    if (!valid_sizes(mode, M, N, K, groups)) return 0;
     Fp8GemmArgs P = {};
     P.M = M;
     P.N = N;
     P.ldc = N;
     P.blocks = (int32_t)(K / FP8_BLOCK);
-    P.groups = mode == FP8_DENSE ? 0 : groups;
+    P.groups = groups;
     const Fp8Choice c = fp8_gemm_choice(P, mode, raw(out_dt), call == 1);
     choice[0] = c.kernel;
     choice[1] = c.rows;

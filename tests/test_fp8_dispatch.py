@@ -35,6 +35,8 @@ def test_which_kernel_serves_a_product(call, M, N, K, groups, dtype, want):
 def test_no_kernel():
     for args in ((0, 4, 128), (4, 0, 128), (4, 4, 100), (4, 4, -128), (1 << 31, 4, 128), (4, 4, (1 << 23) + 128)):
         assert nv.fp8_gemm_kernel("fp8_gemm", *args) is None
+    assert nv.fp8_gemm_kernel("fp8_gemm", (1 << 31) - 1, (1 << 31) - 1, 128) is None and nv.fp8_gemm_kernel("fp8_gemm_experts", 4, 1 << 22, 128, 512) is None
+    assert nv.fp8_gemm_kernel("fp8_gemm_experts_dw", 1 << 22, 4, 128, 512) is None and nv.fp8_gemm_kernel("fp8_gemm_experts_dw", 4, 4, 1 << 30, 2) is None
     for groups in (0, 513):
         assert nv.fp8_gemm_kernel("fp8_gemm_experts", 4, 4, 128, groups) is None and nv.fp8_gemm_kernel("fp8_gemm_experts_dw", 4, 4, 128, groups) is None
     assert L.nvfp4_host_fp8_gemm_kernel(4, 4, 4, 128, 1, nv.BF16, None) == 0 and L.nvfp4_host_fp8_gemm_kernel(0, 4, 4, 128, 1, nv.BF16, None) == 0
