@@ -540,6 +540,88 @@ nvfp4_status nvfp4_moe_combine_bwd(const void *dout, const void *y, nvfp4_dtype 
                                    int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream);
 
 /*
+ * ---- Around the products: the experts' router and its balance, rows' norms, products with packed 4-bit weights
+ *
+ * What a mixture-of-experts block has besides its products and the movement of its rows, forward and backward, and
+ * its products as a program that serves it calls them.  Pointers and pitches of tensors need the alignment of an element only, packed weights 16 bytes.
+ * Outputs share no memory with inputs.  Infinities and NaN go through the formulas.
+ *
+ * nvfp4_moe_route: of each row of logits [tokens, groups] (pitch ld) the top_k largest, ties to the lower expert, in
+ * descending order:
+ *   experts [tokens, top_k]: their numbers; -inf is never chosen: -1 where nothing else is left (nvfp4_moe_sort drops it);
+ *   weights [tokens, top_k]: exp(l - lse), lse = log sum exp over the row, or with renormalize over the chosen; 0 beside -1.
+ * A NaN counts as the largest.  A row that holds a NaN or +inf has NaN among its weights.  groups 1 .. 512, top_k 1 .. groups, tokens * top_k up to 2^31 - 1.
+ */
+nvfp4_status nvfp4_moe_route(const void *logits, nvfp4_dtype dt, int64_t tokens, int32_t groups, int64_t ld, int32_t top_k,
+                             int renormalize, int32_t *experts, float *weights, void *stream);
+/*
+ * How a batch uses the experts.  N = rows of logits with an entry above -inf (others count nowhere), p = softmax of such a
+ * row, lse its logarithm of the sum; experts [tokens, top_k] (integers of id_bytes, 4 or 8; numbers outside 0 .. groups - 1 are
+ * no pair), f[e] = pairs of e / (N top_k), P[e] = sum of p[:, e] / N:
+ *   losses [2]           groups * sum_e f[e] P[e]  (1 where both are even)  and  sum of lse^2 / N  (both 0 without rows);
+ *   counts [groups + 1]  the pairs of each expert, then N;     probs [groups]  P.
+ * The order of the sums follows from the sizes: the same call gives the same bits.  workspace: >=
+ * nvfp4_moe_balance_workspace_bytes(tokens, groups) bytes, 4-byte aligned, NULL where that is 0.
+ */
+size_t nvfp4_moe_balance_workspace_bytes(int64_t tokens, int32_t groups);
+nvfp4_status nvfp4_moe_balance(const void *logits, nvfp4_dtype dt, int64_t tokens, int32_t groups, int64_t ld,
+                               const void *experts, int32_t id_bytes, int32_t top_k, float *losses, int32_t *counts,
+                               float *probs, void *workspace, size_t workspace_bytes, void *stream);
+/*
+ * The gradient of the logits, dlogits [tokens, groups] dense, of their type, rounded once: the sum of
+ *   dweights (NULL: none) [tokens, top_k]: of nvfp4_moe_route's weights for these experts and this renormalize;
+ *   counts, dlosses (both NULL: none): of nvfp4_moe_balance's losses, counts being constants.  counts [groups + 1] may be
+ *     those of several processes' batches added up; each then gets its rows' gradient of the losses of them all.
+ * Rows without an entry above -inf get zeros.  An expert that stands twice in a row counts twice.
+ */
+nvfp4_status nvfp4_moe_route_bwd(const void *logits, nvfp4_dtype dt, int64_t tokens, int32_t groups, int64_t ld, int32_t top_k,
+                                 int renormalize, const int32_t *experts, const float *dweights, const int32_t *counts,
+                                 const float *dlosses, void *dlogits, void *stream);
+
+/*
+ * Norms of the rows of x [rows, cols] (pitch ld):  y = (x - m) r w + b,  r = 1 / sqrt(mean (x - m)^2 + eps),  m the row's mean
+ * (center != 0: layer norm) or 0 (RMS norm).  weight, bias [cols] of weight_dt, NULL for ones and zeros; y dense, of x's
+ * type; mean, rstd: [rows] binary32, NULL where not wanted.  Statistics in binary32, from deviations.  cols up to 2^23; eps >= 0.
+ */
+nvfp4_status nvfp4_layer_norm(const void *x, nvfp4_dtype dt, int64_t rows, int64_t cols, int64_t ld, const void *weight,
+                              const void *bias, nvfp4_dtype weight_dt, int center, float eps, void *y, float *mean, float *rstd,
+                              void *stream);
+/*
+ * Its gradient for dy [rows, cols] (pitch ldy), from x and the saved statistics (mean NULL: the RMS norm's): with
+ * h = (x - mean) rstd and u = dy w,  dx = rstd (u - mean(u) - h mean(u h))  (without mean(u) in an RMS norm), dense;
+ * dweight = sum over rows of dy h and dbias = sum of dy, [cols] of weight_dt, NULL where not wanted; zeros without rows.
+ * Sums in binary32, in an order that follows from the sizes.  workspace: 16-byte aligned, as many bytes as the query says.
+ */
+size_t nvfp4_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols, nvfp4_dtype dt, int dweight, int dbias);
+nvfp4_status nvfp4_layer_norm_bwd(const void *dy, int64_t ldy, const void *x, int64_t ld, nvfp4_dtype dt, int64_t rows, int64_t cols,
+                                  const void *weight, nvfp4_dtype weight_dt, const float *mean, const float *rstd, void *dx,
+                                  void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Products of a tensor that stays as it is with a weight in 4 bits:
+ *   out[i, j] = g sum_k x[i, k] w[j, k],   x [M, K] of x_dt (pitch ldx), w[j, k] the magnitude * scale of W,
+ * W_codes [N, K/2] and W_scales [N, K/block] row-major as nvfp4_quantize writes them, W_scale: device fp32[1], g (not read, may be
+ * NULL, for formats without one).  out [M, N] of out_dt, pitch ldc.  Products are exact, also of binary32 x, and
+ * their sums binary32; g is multiplied in once, at the end, and out rounded once.  The order of the sums follows from the sizes.
+ * Formats as in nvfp4_gemm: E4M3 scales with blocks 16 / 32 / 64 / 128, E8M0 with 32.  K a multiple of 32 and of the block,
+ * up to 2^23; M, N up to 2^31 - 1.  M or N of 0: nothing; K of 0: zeros.  (E8M0: weights under 2^-126 may count as 0.)
+ */
+nvfp4_status nvfp4_gemm_w4(int64_t M, int64_t N, int64_t K, const nvfp4_format *f, const void *x, nvfp4_dtype x_dt, int64_t ldx,
+                           const uint8_t *W_codes, const uint8_t *W_scales, const float *W_scale, void *out, nvfp4_dtype out_dt,
+                           int64_t ldc, void *stream);
+/*
+ * The same by expert: W holds groups * N rows, expert e's N from e N on; offsets (device int32 [groups + 1], ascending from 0 to at
+ * most rows) divides the rows of out [rows, N]; rows of no expert become zeros.
+ *   order  NULL: row r of the product is row r of x, which has x_rows >= rows of them; else device int32 [rows] (nvfp4_moe_sort's): row
+ *          order[r] / top_k of x, zeros where that is negative or past x_rows;
+ *   W_scale  one g for all (W_scale_step 0), or [groups] (1).
+ */
+nvfp4_status nvfp4_gemm_w4_experts(int64_t rows, int64_t N, int64_t K, int32_t groups, const int32_t *offsets, const nvfp4_format *f,
+                                   const void *x, nvfp4_dtype x_dt, int64_t ldx, int64_t x_rows, const int32_t *order, int32_t top_k,
+                                   const uint8_t *W_codes, const uint8_t *W_scales, const float *W_scale, int32_t W_scale_step,
+                                   void *out, nvfp4_dtype out_dt, int64_t ldc, void *stream);
+
+/*
  * Diagnostic, not part of the method: the sustained rate of the matrix
  * instruction a GEMM kernel issues, measured on the current device from a
  * register-only loop (no LDS or global traffic) in that kernel's register-tile

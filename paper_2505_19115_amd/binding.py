@@ -189,6 +189,20 @@ def _load() -> C.CDLL:
     L.nvfp4_moe_combine_bwd.argtypes = [vp, vp, ci, i64, i64, vp, vp, vp, i32, i64, i32, vp, vp, vp]
     L.nvfp4_moe_combine_to_bwd.restype = ci
     L.nvfp4_moe_combine_to_bwd.argtypes = [vp, ci, vp, ci, i64, i64, vp, vp, vp, i32, i64, i32, vp, vp, vp]
+    f32 = C.c_float
+    L.nvfp4_moe_route.restype = L.nvfp4_moe_route_bwd.restype = L.nvfp4_moe_balance.restype = ci
+    L.nvfp4_moe_route.argtypes = [vp, ci, i64, i32, i64, i32, ci, vp, vp, vp]
+    L.nvfp4_moe_route_bwd.argtypes = [vp, ci, i64, i32, i64, i32, ci, vp, vp, vp, vp, vp, vp]
+    L.nvfp4_moe_balance_workspace_bytes.restype = L.nvfp4_layer_norm_bwd_workspace_bytes.restype = sz
+    L.nvfp4_moe_balance_workspace_bytes.argtypes = [i64, i32]
+    L.nvfp4_moe_balance.argtypes = [vp, ci, i64, i32, i64, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    L.nvfp4_layer_norm.restype = L.nvfp4_layer_norm_bwd.restype = ci
+    L.nvfp4_layer_norm.argtypes = [vp, ci, i64, i64, i64, vp, vp, ci, ci, f32, vp, vp, vp, vp]
+    L.nvfp4_layer_norm_bwd_workspace_bytes.argtypes = [i64, i64, ci, ci, ci]
+    L.nvfp4_layer_norm_bwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.nvfp4_gemm_w4.restype = L.nvfp4_gemm_w4_experts.restype = ci
+    L.nvfp4_gemm_w4.argtypes = [i64, i64, i64, fp, vp, ci, i64, vp, vp, vp, vp, ci, i64, vp]
+    L.nvfp4_gemm_w4_experts.argtypes = [i64, i64, i64, i32, vp, fp, vp, ci, i64, i64, vp, i32, vp, vp, vp, i32, vp, ci, i64, vp]
     L.nvfp4_probe_mfma_rate.restype = C.c_int
     L.nvfp4_probe_mfma_rate.argtypes = [C.c_int, C.c_int, C.c_int, vp, C.c_size_t, C.POINTER(C.c_double), vp]
     return L
@@ -227,6 +241,8 @@ EXPORTS = (
     "nvfp4_fp8_codes_bytes", "nvfp4_fp8_scales_bytes", "nvfp4_fp8_slots", "nvfp4_fp8_quantize", "nvfp4_fp8_gemm", "nvfp4_fp8_gemm_workspace_bytes", "nvfp4_fp8_gemm_ws", "nvfp4_fp8_gemm_experts",
     "nvfp4_fp8_gemm_experts_dw", "nvfp4_moe_sort_workspace_bytes", "nvfp4_moe_sort", "nvfp4_moe_gather", "nvfp4_moe_combine", "nvfp4_moe_combine_bwd",
     "nvfp4_moe_combine_to", "nvfp4_moe_combine_to_bwd", "nvfp4_host_fp8_gemm_kernel",
+    "nvfp4_moe_route", "nvfp4_moe_route_bwd", "nvfp4_moe_balance_workspace_bytes", "nvfp4_moe_balance", "nvfp4_layer_norm", "nvfp4_layer_norm_bwd_workspace_bytes",
+    "nvfp4_layer_norm_bwd", "nvfp4_gemm_w4", "nvfp4_gemm_w4_experts",
 )
 
 
@@ -949,3 +965,231 @@ def moe_combine_bwd(dout: torch.Tensor, y: torch.Tensor, weights: torch.Tensor, 
     if code:
         _check(code, "nvfp4_moe_combine_to_bwd")
     return dy, dweights
+
+
+# ---- around the products: the experts' router, rows' norms, packed 4-bit weights
+
+def _device_of(*ts: torch.Tensor | None) -> torch.device:
+    """The device of the first tensor, which is the current one, and that of the others."""
+    index = ts[0].get_device()
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.get_device() != index):
+            raise ValueError("tensors must live on the GPU, all on one")
+    if index != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError("tensors must live on the current device")
+    return ts[0].device
+
+
+def _matrix(x: torch.Tensor, name: str) -> tuple[int, int, int]:
+    """Rows, columns and pitch of a matrix in rows of neighbouring elements."""
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name}: a matrix in rows of neighbouring elements")
+    rows, cols = x.shape
+    ld = x.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name}: rows that do not share elements")
+    return rows, cols, ld
+
+
+def _known(key: tuple, entry, *args) -> int:
+    """A size that the library tells, asked once."""
+    n = _known_sizes.get(key)
+    if n is None:
+        if len(_known_sizes) >= 1000:
+            _known_sizes.clear()
+        n = _known_sizes[key] = entry(*args)
+    return n
+
+
+class MoeRoute(NamedTuple):
+    """What moe_route finds: experts [T, top_k] (int32, -1: none), weights [T, top_k] (float32)."""
+    experts: torch.Tensor
+    weights: torch.Tensor
+
+
+class MoeBalance(NamedTuple):
+    """What moe_balance finds: losses [2] (the balance, the mean lse^2), counts [E + 1] (int32: each expert's pairs, the tokens that count), probs [E]."""
+    losses: torch.Tensor
+    counts: torch.Tensor
+    probs: torch.Tensor
+
+
+class LayerNorm(NamedTuple):
+    """What layer_norm returns: y like x, mean [R] (None without centring) and rstd [R] (float32)."""
+    y: torch.Tensor
+    mean: torch.Tensor | None
+    rstd: torch.Tensor
+
+
+class LayerNormGrads(NamedTuple):
+    """What layer_norm_bwd returns; None for what there was not, or was not wanted."""
+    dx: torch.Tensor
+    dweight: torch.Tensor | None
+    dbias: torch.Tensor | None
+
+
+def _float32(t: torch.Tensor, shape, name: str) -> int:
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.shape != shape:
+        raise TypeError(f"{name}: a contiguous float32 tensor of {tuple(shape)}")
+    return t.data_ptr()
+
+
+def moe_route(logits: torch.Tensor, top_k: int, renormalize: bool = True) -> MoeRoute:
+    """nvfp4_moe_route: logits [T, E] -> each token's top_k experts, ties to the lower one, never one at -inf, and their weights: softmax over the chosen, or
+    (renormalize False) shares of the softmax over all."""
+    device, (T, E, ld) = _device_of(logits), _matrix(logits, "logits")
+    k = top_k if top_k > 0 else 0
+    experts, weights = torch.empty(T, k, dtype=_I32, device=device), torch.empty(T, k, dtype=torch.float32, device=device)
+    code = lib.nvfp4_moe_route(logits.data_ptr(), _dtype_tag(logits), T, E, ld, top_k, renormalize, experts.data_ptr(), weights.data_ptr(), _stream())
+    if code:
+        _check(code, "nvfp4_moe_route")
+    return MoeRoute(experts, weights)
+
+
+def moe_balance(logits: torch.Tensor, experts: torch.Tensor) -> MoeBalance:
+    """nvfp4_moe_balance: logits [T, E], experts [T, top_k] (int32 or int64; numbers outside 0 .. E - 1 are no pair)."""
+    device, (T, E, ld) = _device_of(logits, experts), _matrix(logits, "logits")
+    size = 8 if experts.dtype is torch.int64 else 4
+    if (size == 4 and experts.dtype is not _I32) or not experts.is_contiguous():
+        raise TypeError("experts: a contiguous int32 or int64 tensor")
+    if experts.dim() != 2 or experts.shape[0] != T:
+        raise ValueError(f"experts: [{T}, top_k]")
+    losses, counts, probs = (torch.empty(2, dtype=torch.float32, device=device), torch.empty(E + 1, dtype=_I32, device=device),
+                             torch.empty(E, dtype=torch.float32, device=device))
+    stream, ws_bytes = _stream(), _known(("moe_balance", T, E), lib.nvfp4_moe_balance_workspace_bytes, T, E)
+    block = _Block(ws_bytes, logits, stream) if ws_bytes else None
+    code = lib.nvfp4_moe_balance(logits.data_ptr(), _dtype_tag(logits), T, E, ld, experts.data_ptr(), size, experts.shape[1], losses.data_ptr(), counts.data_ptr(),
+                                 probs.data_ptr(), block.ptr if block else None, ws_bytes, stream)
+    if code:
+        _check(code, "nvfp4_moe_balance")
+    return MoeBalance(losses, counts, probs)
+
+
+def moe_route_bwd(logits: torch.Tensor, experts: torch.Tensor, dweights: torch.Tensor | None = None, renormalize: bool = True, counts: torch.Tensor | None = None,
+                  dlosses: torch.Tensor | None = None) -> torch.Tensor:
+    """nvfp4_moe_route_bwd: the gradient of the logits [T, E] for dweights [T, top_k] of moe_route(logits, top_k, renormalize), which chose these experts
+    (int32), plus that of moe_balance's losses for dlosses [2], with its counts (of one batch, or added up over processes)."""
+    device, (T, E, ld) = _device_of(logits, experts, dweights, counts, dlosses), _matrix(logits, "logits")
+    p_experts = _int32(experts, "experts")
+    if experts.dim() != 2 or experts.shape[0] != T:
+        raise ValueError(f"experts: [{T}, top_k]")
+    if dweights is None and counts is None or (counts is None) != (dlosses is None):
+        raise ValueError("dweights, or counts and dlosses, or all")
+    p_dweights = None if dweights is None else _float32(dweights, experts.shape, "dweights")
+    p_counts, p_dlosses = _int32(counts, "counts"), None if dlosses is None else _float32(dlosses, (2,), "dlosses")
+    if counts is not None and counts.shape != (E + 1,):
+        raise ValueError(f"counts: [{E + 1}]")
+    out = torch.empty(T, E, dtype=logits.dtype, device=device)
+    code = lib.nvfp4_moe_route_bwd(logits.data_ptr(), _dtype_tag(logits), T, E, ld, experts.shape[1], renormalize, p_experts, p_dweights, p_counts, p_dlosses, out.data_ptr(),
+                                   _stream())
+    if code:
+        _check(code, "nvfp4_moe_route_bwd")
+    return out
+
+
+def _per_column(t: torch.Tensor | None, cols: int, name: str) -> int | None:
+    if t is None:
+        return None
+    if t.shape != (cols,) or not t.is_contiguous():
+        raise ValueError(f"{name}: a dense [{cols}]")
+    return t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5, center: bool = True) -> LayerNorm:
+    """nvfp4_layer_norm of the rows of x [R, D]; center False: the RMS norm.  weight, bias: [D] of one type, x's or another."""
+    device, (R, D, ld) = _device_of(x, weight, bias), _matrix(x, "x")
+    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
+        raise TypeError("weight and bias: of one type")
+    w = weight if weight is not None else bias
+    p_weight, p_bias = _per_column(weight, D, "weight"), _per_column(bias, D, "bias")
+    y, rstd = torch.empty(R, D, dtype=x.dtype, device=device), torch.empty(R, dtype=torch.float32, device=device)
+    mean = torch.empty(R, dtype=torch.float32, device=device) if center else None
+    code = lib.nvfp4_layer_norm(x.data_ptr(), _dtype_tag(x), R, D, ld, p_weight, p_bias, F32 if w is None else _dtype_tag(w), center, eps, y.data_ptr(),
+                                mean.data_ptr() if center else None, rstd.data_ptr(), _stream())
+    if code:
+        _check(code, "nvfp4_layer_norm")
+    return LayerNorm(y, mean, rstd)
+
+
+def layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor | None, rstd: torch.Tensor, bias: bool = False) -> LayerNormGrads:
+    """nvfp4_layer_norm_bwd: the gradient of layer_norm for dy like x, from its statistics (mean None: of an RMS norm); bias: whether that of a bias is
+    wanted, which is then of the weight's type (float32 without one)."""
+    device, (R, D, ld) = _device_of(x, dy, weight, mean, rstd), _matrix(x, "x")
+    if dy.shape != x.shape or dy.dtype is not x.dtype:
+        raise ValueError("dy: like x")
+    ldy, p_weight = _matrix(dy, "dy")[2], _per_column(weight, D, "weight")
+    p_mean, p_rstd = None if mean is None else _float32(mean, (R,), "mean"), _float32(rstd, (R,), "rstd")
+    tag = F32 if weight is None else _dtype_tag(weight)
+    dx = torch.empty(R, D, dtype=x.dtype, device=device)
+    dweight = None if weight is None else torch.empty(D, dtype=weight.dtype, device=device)
+    dbias = torch.empty(D, dtype=_torch_dtype(tag), device=device) if bias else None
+    stream, dt = _stream(), _dtype_tag(x)
+    ws_bytes = _known(("layer_norm_bwd", R, D, dt, weight is None, bias), lib.nvfp4_layer_norm_bwd_workspace_bytes, R, D, dt, weight is not None, bool(bias))
+    block = _Block(ws_bytes, x, stream) if ws_bytes else None
+    code = lib.nvfp4_layer_norm_bwd(dy.data_ptr(), ldy, x.data_ptr(), ld, dt, R, D, p_weight, tag, p_mean, p_rstd, dx.data_ptr(), None if dweight is None else dweight.data_ptr(),
+                                    None if dbias is None else dbias.data_ptr(), block.ptr if block else None, ws_bytes, stream)
+    if code:
+        _check(code, "nvfp4_layer_norm_bwd")
+    return LayerNormGrads(dx, dweight, dbias)
+
+
+def _packed_weight(w, K: int, fmt: Format) -> tuple[int, int, int, int | None, int]:
+    """Rows of a packed weight (codes [rows, K / 2], scales [rows, K / block], g), its three addresses, and how many g there are."""
+    codes, scales, g = w
+    if codes.dtype is not _U8 or scales.dtype is not _U8 or not codes.is_contiguous() or not scales.is_contiguous():
+        raise TypeError("a packed weight: contiguous uint8 codes and scales")
+    if codes.dim() != 2 or codes.shape[1] * 2 != K or scales.shape != (codes.shape[0], K // fmt.block):
+        raise ValueError(f"a packed weight: codes [N, {K // 2}] with scales [N, {K // fmt.block}]")
+    if not fmt.tensor_scale:
+        return codes.shape[0], codes.data_ptr(), scales.data_ptr(), None, 1
+    if g is None or g.dtype is not torch.float32 or not g.is_contiguous():
+        raise TypeError("a packed weight's g: contiguous float32")
+    return codes.shape[0], codes.data_ptr(), scales.data_ptr(), g.data_ptr(), g.numel()
+
+
+_formats: dict[Format, _Format] = {}
+
+
+def _format_ref(fmt: Format):
+    f = _formats.get(fmt)
+    if f is None:
+        f = _formats[fmt] = fmt.c()
+    return C.byref(f)
+
+
+def gemm_w4(x: torch.Tensor, w, fmt: Format = NVFP4, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """nvfp4_gemm_w4: x [M, K] as it is against a packed weight w = (codes [N, K / 2], scales [N, K / block], g [1]), quantize's result for [N, K] -> [M, N]."""
+    codes, scales, g = w
+    device, (M, K, ldx) = _device_of(x, codes, scales, g, out), _matrix(x, "x")
+    N, p_codes, p_scales, p_g, ng = _packed_weight(w, K, fmt)
+    if ng != 1:
+        raise ValueError("a packed weight: one g")
+    if out is None:
+        out, ldc = torch.empty(M, N, dtype=out_dtype, device=device), N
+    else:
+        if out.shape != (M, N):
+            raise ValueError(f"out: [{M}, {N}]")
+        ldc = _matrix(out, "out")[2]
+    code = lib.nvfp4_gemm_w4(M, N, K, _format_ref(fmt), x.data_ptr(), _dtype_tag(x), ldx, p_codes, p_scales, p_g, out.data_ptr(), _dtype_tag(out), ldc, _stream())
+    if code:
+        _check(code, "nvfp4_gemm_w4")
+    return out
+
+
+def gemm_w4_experts(x: torch.Tensor, w, offsets: torch.Tensor, fmt: Format = NVFP4, order: torch.Tensor | None = None, top_k: int = 1,
+                    out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """nvfp4_gemm_w4_experts: rows in the experts' order against their experts' rows of a packed [E * N, K] (g: one, or one an expert) -> [R, N].  With order
+    (moe_sort's) and top_k, row r is x[order[r] // top_k]; else x has the rows in that order."""
+    codes, scales, g = w
+    device, (T, K, ldx) = _device_of(x, codes, scales, g, offsets, order), _matrix(x, "x")
+    p_offsets, p_order, groups = _int32(offsets, "offsets"), _int32(order, "order"), offsets.numel() - 1
+    EN, p_codes, p_scales, p_g, ng = _packed_weight(w, K, fmt)
+    if groups < 1 or EN % groups or ng not in (1, groups):
+        raise ValueError(f"a packed weight: [{groups} experts * N, {K}], with one g or one an expert")
+    N, R = EN // groups, T if order is None else order.numel()
+    out = torch.empty(R, N, dtype=out_dtype, device=device)
+    code = lib.nvfp4_gemm_w4_experts(R, N, K, groups, p_offsets, _format_ref(fmt), x.data_ptr(), _dtype_tag(x), ldx, T, p_order, top_k, p_codes, p_scales, p_g, int(ng > 1),
+                                     out.data_ptr(), _dtype_tag(out), N, _stream())
+    if code:
+        _check(code, "nvfp4_gemm_w4_experts")
+    return out
