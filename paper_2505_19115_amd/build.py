@@ -12,7 +12,7 @@ LIB = os.path.join(PKG, "libnvfp4.so")
 SOURCES = ("quantize.hip", "quantize_small.hip", "gemm.hip", "gemm_wide16.hip", "gemm_wide32.hip", "gemm_wide64.hip", "gemm_wide128.hip", "gemm_mx.hip", "gemm_ksplit.hip", "gemm_thin.hip", "fused_small.hip", "probe.hip", "noise.hip", "api.hip",
            "fp8_quantize.hip", "fp8_gemm.hip", "fp8_gemm_thin.hip", "fp8_gemm_wide.hip",
            "moe.hip", "api_experts.hip",
-           "route.hip", "layer_norm.hip", "gemm_w4.hip", "api_layer.hip")
+           "route.hip", "layer_norm.hip", "gemm_w4.hip", "gemm_w4_tiles.hip", "api_layer.hip")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
