@@ -4,7 +4,8 @@ expert's products, and the results back with their weights -- forward and backwa
     python examples/experts_training.py [steps]
 
 Every product of the layer, forward and backward, runs on E4M3 operands with a scale per 128 elements; the weights, the
-activations between the layers and the router stay in the precision they have.
+activations between the layers and the router stay in the precision they have.  The router's choice, its balance over the experts and
+the gradient of both are the library's too, as is the norm of a block's input (RMSNorm).
 """
 import os
 import sys
@@ -48,20 +49,51 @@ class Combine(torch.autograd.Function):
         return (*nv.moe_combine_bwd(dout.contiguous(), y, weights, position, offsets), None, None)
 
 
-class Experts(torch.nn.Module):
-    """SwiGLU experts: out[t] = sum over the token's top_k experts of weight * down(silu(gate(x)) * up(x))."""
+class RMSNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        y, _, rstd = nv.layer_norm(x, weight, center=False)
+        ctx.save_for_backward(x, weight, rstd)
+        return y
 
-    def __init__(self, experts: int, top_k: int, width: int, hidden: int, dtype=torch.bfloat16, device="cuda"):
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, rstd = ctx.saved_tensors
+        return nv.layer_norm_bwd(dy.contiguous(), x, weight, None, rstd)[:2]
+
+
+class Route(torch.autograd.Function):
+    """Each token's experts and their weights, and the losses of how the batch uses the experts: one pass over the logits backward."""
+
+    @staticmethod
+    def forward(ctx, logits, top_k):
+        experts, weights = nv.moe_route(logits, top_k)
+        losses, counts, _ = nv.moe_balance(logits, experts)
+        ctx.save_for_backward(logits, experts, counts)
+        ctx.mark_non_differentiable(experts)
+        return weights, losses, experts
+
+    @staticmethod
+    def backward(ctx, dweights, dlosses, _):
+        logits, experts, counts = ctx.saved_tensors
+        return nv.moe_route_bwd(logits, experts, dweights.contiguous(), counts=counts, dlosses=dlosses.contiguous()), None
+
+
+class Experts(torch.nn.Module):
+    """SwiGLU experts: out[t] = sum over the token's top_k experts of weight * down(silu(gate(x)) * up(x)).  balance: the weight of the balance loss, which forward() leaves in
+    balance_loss."""
+
+    def __init__(self, experts: int, top_k: int, width: int, hidden: int, dtype=torch.bfloat16, device="cuda", balance: float = 0.0):
         super().__init__()
-        self.top_k = top_k
+        self.top_k, self.balance, self.balance_loss = top_k, balance, None
         self.router = torch.nn.Linear(width, experts, bias=False, dtype=torch.float32, device=device)
         make = lambda n, k: torch.nn.Parameter(torch.randn(experts, n, k, device=device).mul_(k ** -0.5).to(dtype))  # noqa: E731
         self.gate_up, self.down = make(2 * hidden, width), make(width, hidden)  # (gate over up: one gather, one product)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        top = torch.topk(self.router(x.float()), self.top_k, dim=1)
-        weights = torch.softmax(top.values, dim=1)
-        offsets, order, position = nv.moe_sort(top.indices, self.down.shape[0])
+        weights, losses, experts = Route.apply(self.router(x.float()), self.top_k)
+        self.balance_loss = self.balance * losses[0]
+        offsets, order, position = nv.moe_sort(experts, self.down.shape[0])
         g, u = ExpertsLinear.apply(x, self.gate_up, offsets, order, position, self.top_k).chunk(2, dim=1)
         y = ExpertsLinear.apply(torch.nn.functional.silu(g) * u, self.down, offsets, None, None, 1)
         return Combine.apply(y, weights, position, offsets)

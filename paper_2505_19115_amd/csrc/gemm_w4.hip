@@ -9,12 +9,16 @@
 
 namespace nvfp4 {
 
-// 16 rows of the output by 16 TN columns a workgroup; its NW waves take the K tiles in turn, and their sums are added through the LDS in the waves' order.
-template <int XDT, int SC, int TN, int NW, bool GROUPED>
+// 16 rows of the output by 16 columns a workgroup; its NW waves take the K tiles in turn, the codes of BATCH of them requested at a time and x of the next one, and their sums are
+// added through the LDS in the waves' order.  us, from memory, NW 4 / 8: 1 x 4096 x 11008 NVFP4 16.3 / 12.9, MXFP4 15.2 / 11.2, 16 x 12288 x 4096 19.8 / 19.7, 4 x 11008 x 2048 8.2 / 9.0, 16 tokens x 2
+// of 8 experts 4096 x 2048 MXFP4 19.8 / 24.2, 1 x 2 6.8 / 7.1, 8 x 2 of 64 1024 x 1024 7.6 / 9.9: eight where there are few columns.  The floor of the first is 4.8 us: a wave takes 0.5 us and more
+// for a K tile, whatever there is to load (1 x 256 x 12288, 1.7 MB, 11.8).  Tried: twelve K tiles' codes at a time and x of four (12.3, experts 25), four waves on columns of their own instead
+// of parts of the contraction (experts 25).
+template <int XDT, int SC, int NW, bool GROUPED>
 __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
 {
     using namespace w4;
-    constexpr int MT = 1, ROWS = 16 * MT, COLS = 16 * TN, XSZ = Elem<XDT>::BYTES;
+    constexpr int BATCH = 4, ROWS = 16, COLS = 16, XSZ = Elem<XDT>::BYTES;
     __shared__ float sums[NW][ROWS][COLS + 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, r = lane & 15;
     // workgroups side by side take the same columns
@@ -33,63 +37,61 @@ __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
     if (count > ROWS) count = ROWS;
     const bool none = GROUPED && e == P.groups;  // rows of no group
     const int shift = SC == TWO_E4M3 ? 4 : 31 - __builtin_clz((unsigned)P.block);
-    const uint8_t *codes[TN], *scales[TN], *x[MT];
+    int64_t w_row = n0 + r;
+    w_row = (w_row < P.N ? w_row : P.N - 1) + (none ? 0 : e) * P.N;
+    const uint8_t *const codes = P.codes + w_row * (P.K >> 1), *const scales = P.scales + w_row * (P.K >> shift);
+    // W's first batch is on its way before an order says which rows of x there are
+    const int tiles = none ? 0 : (int)((P.K + 127) >> 7);
+    Codes<SC> a[BATCH];
+    auto load_w = [&](int kt) {
 #pragma unroll
-    for (int t = 0; t < TN; ++t) {
-        int64_t row = n0 + t * 16 + r;
-        row = (row < P.N ? row : P.N - 1) + (none ? 0 : e) * P.N;
-        codes[t] = P.codes + row * (P.K >> 1) + q * 16;
-        scales[t] = P.scales + row * (P.K >> shift);
-    }
-    bool row_there[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        int64_t row = t * 16 + r;
-        row_there[t] = row < count && !none;
-        row = row_there[t] ? m0 + row : 0;
-        if (GROUPED && P.order && row_there[t]) {
+        for (int u = 0; u < BATCH; ++u) {
+            const int64_t k = (int64_t)(kt + u * NW) * 128 + q * 32;
+            if (kt + u * NW < tiles) a[u].load(codes + (k < P.K ? k >> 1 : 0), scales + (k < P.K ? k >> shift : 0), true);
+        }
+    };
+    load_w(wave);
+    const uint8_t *x;
+    bool row_there = r < count && !none;
+    {
+        int64_t row = row_there ? m0 + r : 0;
+        if (GROUPED && P.order && row_there) {
             const int32_t pair = P.order[row];
             row = pair < 0 ? -1 : pair / P.top_k;
-            row_there[t] = row >= 0 && row < P.x_rows;
-            if (!row_there[t]) row = 0;
+            row_there = row >= 0 && row < P.x_rows;
+            if (!row_there) row = 0;
         }
-        x[t] = P.x + (row * P.ldx + q * 32) * XSZ;
+        x = P.x + (row * P.ldx + q * 32) * XSZ;
     }
-    float4v_t acc[MT][TN];
+    float4v_t acc = {0, 0, 0, 0};
+    for (int kt = wave; kt < tiles; kt += NW * BATCH) {
+        if (kt != wave) load_w(kt);
+        Elems<XDT> b[2];
+        auto load_x = [&](int u) {
+            const int64_t k = (int64_t)(kt + u * NW) * 128;
+            b[u & 1].load(x + k * XSZ, row_there && k + q * 32 < P.K);
+        };
+        load_x(0);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int u = 0; u < BATCH; ++u) {
+            if (kt + u * NW >= tiles) break;
+            if (u + 1 < BATCH) load_x(u + 1);
+            const bool there = (int64_t)(kt + u * NW) * 128 + q * 32 < P.K;  // (past the end came some codes of the row)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = float4v_t{0, 0, 0, 0};
-    const int tiles = none ? 0 : (int)((P.K + 127) >> 7);
-    for (int kt = wave; kt < tiles; kt += NW) {
-        const int64_t k = (int64_t)kt * 128;
-        const bool there = k + q * 32 < P.K;
-        Codes<SC> a[TN];
-        Elems<XDT> b[MT];
+            for (int i = 0; i < 4; ++i) a[u].w[i] = there ? a[u].w[i] : 0;
+            a[u].s = there ? a[u].s : 0;
 #pragma unroll
-        for (int t = 0; t < TN; ++t) a[t].load(codes[t] + (k >> 1), scales[t] + ((k + q * 32) >> shift), there);
+            for (int p = 0; p < 4; ++p) {
+                bf16x8_t fb[Elems<XDT>::PIECES];
+                b[u & 1].part(p, fb);
+                const bf16x8_t fa = a[u].part(p);
 #pragma unroll
-        for (int t = 0; t < MT; ++t) b[t].load(x[t] + k * XSZ, there && row_there[t]);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            bf16x8_t fb[MT][Elems<XDT>::PIECES];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) b[i].part(p, fb[i]);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                const bf16x8_t fa = a[j].part(p);
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int s = 0; s < Elems<XDT>::PIECES; ++s) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[i][s], acc[i][j], 0, 0, 0);
+                for (int s = 0; s < Elems<XDT>::PIECES; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[s], acc, 0, 0, 0);
             }
         }
     }
     // lane (q, r) has columns 4 q .. 4 q + 3 of row r
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) *reinterpret_cast<float4v_t *>(&sums[wave][i * 16 + r][j * 16 + q * 4]) = acc[i][j];
+    *reinterpret_cast<float4v_t *>(&sums[wave][r][q * 4]) = acc;
     __syncthreads();
     const float g = P.g ? P.g[none ? 0 : e * P.g_step] : 1.0f;
     for (int id = threadIdx.x; id < ROWS * COLS; id += 64 * NW) {
@@ -105,19 +107,22 @@ __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
 
 namespace w4 {
 
-template <int XDT, int SC>
-static hipError_t few_rows(W4Args P, int out_dt, hipStream_t st)
+template <int XDT, int SC, int NW>
+static hipError_t divided(W4Args P, int64_t slots, int out_dt, hipStream_t st)
 {
-    constexpr int TN = 1, NW = 8;
-    const int64_t cols = (P.N + 16 * TN - 1) / (16 * TN);
-    if (P.groups > 0) {
-        P.slots = (uint32_t)(P.rows / 16 + (P.rows < P.groups + 1 ? P.rows : P.groups + 1));
-        gemm_w4_kernel<XDT, SC, TN, NW, true><<<launch_grid(cols * P.slots), 64 * NW, 0, st>>>(P, out_dt);
-    } else {
-        P.slots = 1;
-        gemm_w4_kernel<XDT, SC, TN, NW, false><<<launch_grid(cols * P.slots), 64 * NW, 0, st>>>(P, out_dt);
-    }
+    P.slots = (uint32_t)slots;
+    const dim3 grid = launch_grid((P.N + 15) / 16 * slots);
+    if (P.groups > 0) gemm_w4_kernel<XDT, SC, NW, true><<<grid, 64 * NW, 0, st>>>(P, out_dt);
+    else gemm_w4_kernel<XDT, SC, NW, false><<<grid, 64 * NW, 0, st>>>(P, out_dt);
     return hipGetLastError();
+}
+
+constexpr int64_t MANY = 512;  // workgroups that fill the CUs with four waves each
+template <int XDT, int SC>
+static hipError_t few_rows(const W4Args &P, int out_dt, hipStream_t st)
+{
+    const int64_t slots = P.groups > 0 ? P.rows / 16 + (P.rows < P.groups + 1 ? P.rows : P.groups + 1) : 1;
+    return (P.N + 15) / 16 * slots >= MANY ? divided<XDT, SC, 4>(P, slots, out_dt, st) : divided<XDT, SC, 8>(P, slots, out_dt, st);
 }
 
 }  // namespace w4

@@ -5,6 +5,8 @@
 //   bwd      of weights over the chosen: dl_e = w_e (dw_e - sum_i w_i dw_i);  over the row: p_e (dw_e - sum_i w_i dw_i), dw_e = 0 where e is not chosen;
 //            of the balance: dL0 (E / N) p_e (f_e - sum_i f_i p_i), f taken as constants;  of lse^2: dL1 (2 / N) lse p_e
 // G lanes hold a row, eight entries each, so that a row of up to 512 experts is in registers and read once.
+// us, kernels alone: route 16 x 8 2.8 (a launch), 32768 x 128 bf16 k 8 10.8: eight rounds of some 50 instructions, where its 8 MB take 1.6; bwd 32768 x 128 binary32 with both gradients
+// 16.2 (34 MB: 6.3 at a copy's rate; the rest exponentials and finding the choices' lanes); balance 32768 x 256 bf16 13.6 + 10 (17 MB: 3.2).
 #include <math.h>
 
 #include "layer_ops.h"
@@ -88,7 +90,7 @@ __global__ __launch_bounds__(256) void moe_route_kernel(const uint8_t *logits, i
         for (int i = 0; i < V; ++i) sum += expf(v[i] - top);
         sum = group_sum<G>(sum);
     }
-    extern __shared__ float staged[];  // what the weights are before they are divided: [256 / G][top_k]
+    extern __shared__ float staged[];  // the chosen logits: [256 / G][top_k]
     float *const mine = staged + threadIdx.x / G * top_k;
     for (int j = 0; j < top_k; ++j) {
         if (j > 0) {
@@ -103,21 +105,34 @@ __global__ __launch_bounds__(256) void moe_route_kernel(const uint8_t *logits, i
         for (int i = V - 1; i >= 0; --i)
             if (key[i] == most) first = i;
         const uint64_t have = __ballot(first < V) >> (lane & ~(G - 1));
-        const bool wins = __builtin_ctzll(have) == (lane & (G - 1));
-        const float e = chosen ? expf(of_key(most) - top) : 0.0f;
-        if (renormalize) sum += e;
+        const bool wins = __builtin_ctzll(have) == g;
         if (wins && there) {
             experts[t * top_k + j] = chosen ? g * V + first : -1;
-            mine[j] = chosen ? e : -1.0f;
+            mine[j] = chosen ? of_key(most) : NONE;
         }
+        if (wins && chosen) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (wins && chosen && i == first) key[i] = 0;
+            for (int i = 0; i < V; ++i)
+                if (i == first) key[i] = 0;
+        }
     }
     __syncthreads();
+    // the row's lanes share its choices; the exponentials once, outside the rounds
+    const float mark = NONE;
+    if (renormalize) {
+        for (int j = g; j < top_k; j += G) {
+            const float l = there ? mine[j] : mark;
+            const float e = l == mark ? 0.0f : expf(l - top);
+            if (there && l != mark) mine[j] = e;
+            if (there && l == mark) mine[j] = -1.0f;
+            sum += e;
+        }
+        sum = group_sum<G>(sum);
+    }
     if (!there) return;
     for (int j = g; j < top_k; j += G) {
-        const float e = mine[j];
+        float e = mine[j];
+        if (!renormalize) e = e == mark ? -1.0f : expf(e - top);
         weights[t * top_k + j] = e < 0.0f ? 0.0f : e / sum;
     }
 }
@@ -138,15 +153,25 @@ __global__ __launch_bounds__(256) void moe_route_bwd_kernel(const uint8_t *logit
     if (dweights) {
 #pragma unroll
         for (int i = 0; i < V; ++i) up[i] = times[i] = 0.0f;
-        for (int j = 0; j < top_k; ++j) {
-            const int at = experts[t * top_k + j] - g * V;
-            const float dw = dweights[t * top_k + j];
+        for (int j0 = 0; j0 < top_k; j0 += 8) {  // (loads of eight choices at a time)
+            int at[8];
+            float dw[8];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (at == i && g * V + i < groups) {
-                    up[i] += dw;
-                    times[i] += 1.0f;
-                }
+            for (int u = 0; u < 8; ++u) {
+                const int64_t j = t * top_k + (j0 + u < top_k ? j0 + u : 0);
+                at[u] = experts[j];
+                dw[u] = dweights[j];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                at[u] = j0 + u < top_k && (unsigned)at[u] < (unsigned)groups ? at[u] - g * V : -1;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (at[u] == i) {
+                        up[i] += dw[u];
+                        times[i] += 1.0f;
+                    }
+            }
         }
         if (renormalize) {
             uint32_t most = 0;
@@ -319,9 +344,21 @@ __global__ __launch_bounds__(1024) void moe_balance_end_kernel(const float *part
     if (slice < slices) {
         float s = 0.0f;
         int c = 0;
-        for (int p = slice; p < parts; p += slices) {
-            s += part_sums[(int64_t)p * cells + e];
-            c += part_counts[(int64_t)p * cells + e];
+        for (int p0 = slice; p0 < parts; p0 += 16 * slices) {  // (loads of sixteen parts at a time: one after the other took 25 us of 38)
+            float v[16];
+            int n[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                const int64_t at = (int64_t)(p0 + u * slices < parts ? p0 + u * slices : slice) * cells + e;
+                v[u] = part_sums[at];
+                n[u] = part_counts[at];
+            }
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                if (p0 + u * slices < parts) {
+                    s += v[u];
+                    c += n[u];
+                }
         }
         sums[tid] = s;
         hist[tid] = c;
