@@ -604,7 +604,8 @@ nvfp4_status nvfp4_layer_norm_bwd(const void *dy, int64_t ldy, const void *x, in
  * NULL, for formats without one).  out [M, N] of out_dt, pitch ldc.  Products are exact, also of binary32 x, and
  * their sums binary32; g is multiplied in once, at the end, and out rounded once.  The order of the sums follows from the sizes.
  * Formats as in nvfp4_gemm: E4M3 scales with blocks 16 / 32 / 64 / 128, E8M0 with 32.  K a multiple of 32 and of the block,
- * up to 2^23; M, N up to 2^31 - 1.  M or N of 0: nothing; K of 0: zeros.  (E8M0: weights under 2^-126 may count as 0.)
+ * up to 2^23; M, N up to 2^31 - 1.  M or N of 0: nothing; K of 0: zeros.  (Weights and parts of a binary32 x under 2^-126 may
+ * count as 0; without g the sums have to stay inside binary32.)
  */
 nvfp4_status nvfp4_gemm_w4(int64_t M, int64_t N, int64_t K, const nvfp4_format *f, const void *x, nvfp4_dtype x_dt, int64_t ldx,
                            const uint8_t *W_codes, const uint8_t *W_scales, const float *W_scale, void *out, nvfp4_dtype out_dt,
