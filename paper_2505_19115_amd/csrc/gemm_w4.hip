@@ -63,6 +63,8 @@ __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
         }
         x = P.x + (row * P.ldx + q * 32) * XSZ;
     }
+    // (the same in every wave: lane r asks for row r)  Rows that are not there become zeros whatever W and g hold
+    const uint64_t rows_there = __ballot(row_there);
     float4v_t acc = {0, 0, 0, 0};
     for (int kt = wave; kt < tiles; kt += NW * BATCH) {
         if (kt != wave) load_w(kt);
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
         if (m >= count || n0 + n >= P.N) continue;
         float s = sums[0][m][n];
         for (int w = 1; w < NW; ++w) s += sums[w][m][n];
-        s = none ? 0.0f : s * g;
+        s = rows_there >> m & 1 ? s * g : 0.0f;
         if (out_dt == NVFP4_BF16) Elem<NVFP4_BF16>::store(P.out + ((m0 + m) * P.ldc + n0 + n) * 2, s);
         else Elem<NVFP4_F32>::store(P.out + ((m0 + m) * P.ldc + n0 + n) * 4, s);
     }

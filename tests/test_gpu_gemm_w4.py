@@ -227,3 +227,28 @@ def test_empty_and_refusals():
     with pytest.raises(nv.Nvfp4Error):
         nv.gemm_w4_experts(x, w, o, order=o, top_k=0)
     assert nv.gemm_w4_experts(x[:0], w, torch.zeros(3, dtype=torch.int32, device="cuda")).shape == (0, 16)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("each", [1, 9, 16, 17, 40, 130])
+def test_rows_that_an_order_does_not_name_are_zeros(each, dtype):
+    # whatever their expert's weight holds, in the kernel for few rows (up to 16 an expert) and in tiles: NaN scale bytes, a g that is infinite or NaN
+    E, N, K, T, k = 3, 50, 384, 21, 3
+    codes, scales, _ = packed(E * N, K, nv.NVFP4)
+    scales[N: 2 * N] = 0x7F
+    g = torch.tensor([1.0, 1.0, float("inf")], device="cuda")
+    x = activation(T, K, dtype).cuda()
+    rows = E * each
+    order = torch.randint(0, T * k, (rows,), generator=torch.Generator().manual_seed(each)).int()
+    order[::2] = -1
+    order[::6] = T * k + 4
+    offsets = offsets_of([each] * E, rows).cuda()
+    named = ((order >= 0) & (order < T * k)).cuda()
+    for out in DTYPES:
+        got = nv.gemm_w4_experts(x, (codes, scales, g), offsets, order=order.cuda(), top_k=k, out_dtype=out)
+        assert not torch.isnan(got[~named]).any() and not got[~named].any()
+        second = torch.arange(rows, device="cuda") // each == 1
+        assert torch.isnan(got[named & second]).all() and torch.isfinite(got[:each]).all()
+        # g alone is not a number: the products of x that are zeros are
+        got = nv.gemm_w4_experts(x, (codes, scales, g[2:] * 0), offsets, order=order.cuda(), top_k=k, out_dtype=out)
+        assert not torch.isnan(got[~named]).any() and not got[~named].any() and torch.isnan(got[named]).all()
