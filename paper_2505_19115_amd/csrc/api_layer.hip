@@ -150,7 +150,7 @@ static nvfp4_status product_w4(int64_t rows, int64_t N, int64_t K, int32_t group
     P.K = K;
     P.codes = codes;
     P.scales = scales;
-    P.g = f->tensor_scale ? g : nullptr;
+    P.g = f->tensor_scale && K > 0 ? g : nullptr;  // (a sum of nothing is 0 whatever g is)
     P.g_step = g_step;
     P.block = f->block;
     P.scale = f->scale;

@@ -252,3 +252,14 @@ def test_rows_that_an_order_does_not_name_are_zeros(each, dtype):
         # g alone is not a number: the products of x that are zeros are
         got = nv.gemm_w4_experts(x, (codes, scales, g[2:] * 0), offsets, order=order.cuda(), top_k=k, out_dtype=out)
         assert not torch.isnan(got[~named]).any() and not got[~named].any() and torch.isnan(got[named]).all()
+
+
+@pytest.mark.parametrize("g", [float("inf"), float("nan")])
+@pytest.mark.parametrize("M", [1, 16, 17, 140])
+def test_a_sum_of_nothing_is_zero_whatever_g_is(M, g):
+    x = torch.randn(M, 32, device="cuda")[:, :0]
+    w = (torch.empty(6, 0, dtype=torch.uint8, device="cuda"), torch.empty(6, 0, dtype=torch.uint8, device="cuda"), torch.tensor([g], device="cuda"))
+    for out in DTYPES:
+        got = nv.gemm_w4(x, w, out_dtype=out)
+        assert got.shape == (M, 6) and (got == 0).all()
+        assert (nv.gemm_w4_experts(x, w, torch.tensor([0, M, M], dtype=torch.int32, device="cuda"), out_dtype=out) == 0).all()
