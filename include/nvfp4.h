@@ -582,6 +582,7 @@ nvfp4_status nvfp4_moe_route_bwd(const void *logits, nvfp4_dtype dt, int64_t tok
  * Norms of the rows of x [rows, cols] (pitch ld):  y = (x - m) r w + b,  r = 1 / sqrt(mean (x - m)^2 + eps),  m the row's mean
  * (center != 0: layer norm) or 0 (RMS norm).  weight, bias [cols] of weight_dt, NULL for ones and zeros; y dense, of x's
  * type; mean, rstd: [rows] binary32, NULL where not wanted.  Statistics in binary32, from deviations.  cols up to 2^23; eps >= 0.
+ * rows or cols of 0: nothing is written, no statistics either.
  */
 nvfp4_status nvfp4_layer_norm(const void *x, nvfp4_dtype dt, int64_t rows, int64_t cols, int64_t ld, const void *weight,
                               const void *bias, nvfp4_dtype weight_dt, int center, float eps, void *y, float *mean, float *rstd,

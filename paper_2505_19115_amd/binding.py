@@ -1096,7 +1096,7 @@ def _per_column(t: torch.Tensor | None, cols: int, name: str) -> int | None:
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5, center: bool = True) -> LayerNorm:
-    """nvfp4_layer_norm of the rows of x [R, D]; center False: the RMS norm.  weight, bias: [D] of one type, x's or another."""
+    """nvfp4_layer_norm of the rows of x [R, D]; center False: the RMS norm.  weight, bias: [D] of one type, x's or another.  D of 0: statistics of NaN."""
     device, (R, D, ld) = _device_of(x, weight, bias), _matrix(x, "x")
     if weight is not None and bias is not None and weight.dtype is not bias.dtype:
         raise TypeError("weight and bias: of one type")
@@ -1104,6 +1104,10 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     p_weight, p_bias = _per_column(weight, D, "weight"), _per_column(bias, D, "bias")
     y, rstd = torch.empty(R, D, dtype=x.dtype, device=device), torch.empty(R, dtype=torch.float32, device=device)
     mean = torch.empty(R, dtype=torch.float32, device=device) if center else None
+    if D == 0:  # (the call writes nothing; a mean of nothing is 0 / 0)
+        rstd.fill_(float("nan"))
+        if center:
+            mean.fill_(float("nan"))
     code = lib.nvfp4_layer_norm(x.data_ptr(), _dtype_tag(x), R, D, ld, p_weight, p_bias, F32 if w is None else _dtype_tag(w), center, eps, y.data_ptr(),
                                 mean.data_ptr() if center else None, rstd.data_ptr(), _stream())
     if code:

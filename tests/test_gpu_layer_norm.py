@@ -221,3 +221,15 @@ def test_no_rows_and_refusals():
         nv.layer_norm_bwd(x, x, w, s.mean[:3], s.rstd)
     with pytest.raises(TypeError):
         nv.layer_norm_bwd(x, x, w, s.mean, s.rstd.double())
+
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_statistics_of_rows_without_columns(dtype, center):
+    # a mean of nothing is 0 / 0, and so is what follows from it; never what the memory held before
+    for R in (1, 5, 300):
+        torch.full((4, R), 7.0, device="cuda")  # (freed at once: the next tensors of this size are made of it)
+        got = nv.layer_norm(torch.empty(R, 0, dtype=dtype, device="cuda"), center=center)
+        assert got.y.shape == (R, 0) and torch.isnan(got.rstd).all() and (torch.isnan(got.mean).all() if center else got.mean is None)
+        grads = nv.layer_norm_bwd(got.y, got.y, torch.empty(0, device="cuda"), got.mean, got.rstd, bias=True)
+        assert grads.dx.shape == (R, 0) and grads.dweight.shape == grads.dbias.shape == (0,)
