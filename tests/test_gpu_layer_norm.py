@@ -233,3 +233,32 @@ def test_statistics_of_rows_without_columns(dtype, center):
         assert got.y.shape == (R, 0) and torch.isnan(got.rstd).all() and (torch.isnan(got.mean).all() if center else got.mean is None)
         grads = nv.layer_norm_bwd(got.y, got.y, torch.empty(0, device="cuda"), got.mean, got.rstd, bias=True)
         assert grads.dx.shape == (R, 0) and grads.dweight.shape == grads.dbias.shape == (0,)
+
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("D, R", [(16391, 4096), (65537, 8192), (262147, 2048)])
+def test_column_sums_of_long_rows(D, R, center):
+    # numbers of one sign, where every rounding of a chain of additions may fall the same way.  A term dy (x - m) r is off by 3 u, its column's sums inside a thread by 2 u (they carry what
+    # their roundings leave), the 16 at most of a column's workgroups by 16 u, the result by u
+    x = torch.rand(R, D, generator=torch.Generator(device="cuda").manual_seed(D), device="cuda") + 0.5
+    dy = torch.full((R, D), 0.1, device="cuda")
+    m, r = torch.full((R,), -0.25, device="cuda"), torch.full((R,), 0.7, device="cuda")
+    got = nv.layer_norm_bwd(dy, x, torch.ones(D, device="cuda"), m if center else None, r, bias=True)
+    db = float(dy[0, 0].double()) * R
+    assert ((got.dbias.double() / db - 1).abs() <= 19 * U).all()
+    dw = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for part in x.split(256):
+        dw += (part.double() - (m[0].double() if center else 0)).mul_(r[0].double() * dy[0, 0].double()).sum(0)
+    assert ((got.dweight.double() / dw - 1).abs() <= 22 * U).all()
+
+
+def test_column_sums_of_long_rows_keep_infinities():
+    D, R = 16391, 300
+    x, dy = torch.ones(R, D, device="cuda"), torch.ones(R, D, device="cuda")
+    dy[7, 5], dy[8, 6], dy[9, 6], dy[100, 16390] = float("inf"), float("inf"), -float("inf"), -float("inf")
+    dy[40, 9] = dy[200, 9] = dy[40, 10] = dy[41, 10] = 3e38
+    got = nv.layer_norm_bwd(dy, x, torch.ones(D, device="cuda"), None, torch.ones(R, device="cuda"), bias=True)
+    for v in (got.dweight, got.dbias):
+        assert v[5] == float("inf") and torch.isnan(v[6]) and v[16390] == -float("inf") and v[9] == v[10] == float("inf")
+        v[[5, 6, 9, 10, 16390]] = R
+        assert (v == R).all()
