@@ -284,18 +284,37 @@ __global__ __launch_bounds__(BALANCE_NT) void moe_balance_kernel(const uint8_t *
         const ID e = experts[i];
         if (e >= 0 && e < (ID)groups) atomicAdd(&hist[(int)e], 1);
     }
-    float sum[V], squares = 0.0f;
+    // sums of 64 rows, of 64 of these, of those: a chain of thousands of additions in a long batch would lose ten bits
+    float sum[V + 1], some[V + 1], most[V + 1];  // (lse^2 behind the probabilities)
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+    for (int i = 0; i <= V; ++i) sum[i] = some[i] = most[i] = 0.0f;
     int kept = 0;
+    unsigned step = 0;
     for (int64_t t = first + tid / G; t < last; t += ROWS) {
         float v[V], lse;
         load_row<DT, G>(v, logits, ld, t, groups, true);
         kept += softmax<G>(v, &lse);
-        squares += lse * lse;
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += v[i];
+        sum[V] += lse * lse;
+        if ((++step & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i <= V; ++i) {
+                some[i] += sum[i];
+                sum[i] = 0.0f;
+            }
+            if ((step & 4095) == 0) {
+#pragma unroll
+                for (int i = 0; i <= V; ++i) {
+                    most[i] += some[i];
+                    some[i] = 0.0f;
+                }
+            }
+        }
     }
+#pragma unroll
+    for (int i = 0; i <= V; ++i) sum[i] += some[i] + most[i];
+    float squares = sum[V];
     // the wave's rows, then the waves'
 #pragma unroll
     for (int d = G; d < 64; d <<= 1) {

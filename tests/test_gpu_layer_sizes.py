@@ -1,10 +1,13 @@
-"""Offsets past 32 bits: the last rows of tensors of more than 2^32 bytes, against calls on these rows alone (the same kernels, the same bits)."""
+"""Offsets past 32 bits: the last rows of tensors of more than 2^32 bytes, against calls on these rows alone (the same kernels, the same bits); sums over long batches."""
+import math
+
 import pytest
 import torch
 
 from paper_2505_19115_amd import binding as nv
 
 pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
 
 
 def test_route_and_gradient():
@@ -47,3 +50,16 @@ def test_packed_products(dtype):
     y = nv.gemm_w4(x, one, out_dtype=torch.float32)
     few = nv.gemm_w4(x[-300:], one, out_dtype=torch.float32)
     assert not y[:-300].any() and ((y[-300:] - few).abs() <= 1e-5 * few.abs().max()).all()
+
+
+def test_balance_of_a_long_batch():
+    # 2^23 tokens, 4096 for each group of lanes, all alike: every rounding of a chain of additions falls the same way.  Sums of 64, of 64 of these, of those; then 3 lanes' groups,
+    # 8 waves and 256 parts (in three slices): 64 + 64 + 1 + 3 + 8 + 86 + 3 additions at most one after the other, 12 u for a share
+    T, E = 1 << 23, 290
+    l = torch.zeros(T, E, dtype=torch.bfloat16, device="cuda")
+    got = nv.moe_balance(l, torch.zeros(T, 1, dtype=torch.int32, device="cuda"))
+    bound = (64 + 64 + 1 + 3 + 8 + 86 + 3 + 12) * U
+    assert got.counts.tolist() == [T] + [0] * (E - 1) + [T]
+    assert ((got.probs.double() * E - 1).abs() <= bound).all() and abs(float(got.losses[0]) - 1) <= bound + (E + 20) * U
+    size = math.log(E) ** 2
+    assert abs(float(got.losses[1]) / size - 1) <= bound + 12 * U
