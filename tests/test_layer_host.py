@@ -1,11 +1,17 @@
 """CPU-only checks of the host side of the router, the norms and the products with packed 4-bit weights: sizes, and every refusal of the C ABI, which
 happens before anything is launched (pointers here are numbers that nobody follows)."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
 
 from paper_2505_19115_amd import binding as nv
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CLANG = "/opt/rocm/lib/llvm/bin/clang++"
 
 L = nv.lib
 P, Q = 0x10000, 0x20000  # 16-byte aligned
@@ -146,3 +152,11 @@ def test_binding_refuses_tensors_off_the_gpu():
                  lambda: nv.layer_norm_bwd(x, x, None, None, torch.ones(4)), lambda: nv.gemm_w4(x, w), lambda: nv.gemm_w4_experts(x, w, ids[0])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.skipif(not shutil.which(CLANG), reason="needs the ROCm compilers")
+def test_launches_count_their_threads_in_32_bits(tmp_path):
+    exe = str(tmp_path / "launch_grid")
+    subprocess.check_call([CLANG, "-std=c++17", "-O1", "-x", "hip", "--offload-host-only", "-I/opt/rocm/include", "-o", exe, os.path.join(ROOT, "tests", "launch_grid_main.cpp"), "-L/opt/rocm/lib", "-lamdhip64"])
+    p = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert p.returncode == 0 and "grids ok" in p.stdout, p.stderr
