@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void moe_route_bwd_kernel(const uint8_t *logit
     }
     if (counts || (dweights && !renormalize)) {
         float lse;
-        softmax<G>(l, &lse);
+        const bool kept = softmax<G>(l, &lse);
         if (dweights && !renormalize) {
             float dot = 0.0f;
 #pragma unroll
@@ -211,8 +211,8 @@ __global__ __launch_bounds__(256) void moe_route_bwd_kernel(const uint8_t *logit
             for (int i = 0; i < V; ++i) d[i] = l[i] * (up[i] - dot);
         }
         if (counts) {
-            const int kept = counts[groups];
-            const float n = kept > 1 ? (float)kept : 1.0f, per = 1.0f / (n * (float)top_k);
+            const int rows = counts[groups];
+            const float n = rows > 1 ? (float)rows : 1.0f, per = 1.0f / (n * (float)top_k);
             float f[V], dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -224,6 +224,9 @@ __global__ __launch_bounds__(256) void moe_route_bwd_kernel(const uint8_t *logit
 #pragma unroll
             for (int i = 0; i < V; ++i) d[i] += l[i] * (a * (f[i] - dot) + b);
         }
+        // (also where what comes back is not a number: 0 times it is none either)
+#pragma unroll
+        for (int i = 0; i < V; ++i) d[i] = kept ? d[i] : 0.0f;
     }
     store_run<DT, V>(d, dlogits + (t * groups + g * V) * Elem<DT>::BYTES, groups - g * V);
 }

@@ -308,3 +308,22 @@ def test_empty_and_refusals():
         nv.moe_route_bwd(l, r.experts, r.weights.double())
     with pytest.raises(TypeError):
         nv.moe_route_bwd(l, r.experts.long(), r.weights)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("E", [5, 100])
+def test_gradient_of_padding_is_zero_whatever_comes_back(E, dtype, renormalize, bad):
+    # a scaled loss that has overflown must not reach the rows that count nowhere
+    l = drawn(E, 40, E, dtype, "none")
+    l[::3] = -math.inf
+    r = nv.moe_route(l.cuda(), 2, renormalize=renormalize)
+    counts, dw = nv.moe_balance(l.cuda(), r.experts).counts, torch.full((40, 2), bad, device="cuda")
+    for dlosses in ([bad, 0.0], [0.0, bad], [bad, bad]):
+        for experts in (r.experts, torch.zeros_like(r.experts)):  # (also where a list names an expert for a row that has none)
+            for weights in (None, dw):
+                d = nv.moe_route_bwd(l.cuda(), experts, weights, renormalize=renormalize, counts=counts, dlosses=torch.tensor(dlosses, device="cuda"))
+                assert (d[::3] == 0).all() and not torch.isfinite(d[1::3]).all()
+                d = nv.moe_route_bwd(l.cuda(), experts, dw, renormalize=renormalize)
+                assert (d[::3] == 0).all()
