@@ -4,8 +4,8 @@ expert's products, and the results back with their weights -- forward and backwa
     python examples/experts_training.py [steps]
 
 Every product of the layer, forward and backward, runs on E4M3 operands with a scale per 128 elements; the weights, the
-activations between the layers and the router stay in the precision they have.  The router's choice, its balance over the experts and
-the gradient of both are the library's too, as is the norm of a block's input (RMSNorm).
+activations between the layers and the router stay in the precision they have.  The router's choice, its balance over the experts where that
+has a weight, and the gradient of both are the library's too; RMSNorm, for a block's input, has the library's norm and its gradient.
 """
 import os
 import sys
@@ -63,12 +63,12 @@ class RMSNorm(torch.autograd.Function):
 
 
 class Route(torch.autograd.Function):
-    """Each token's experts and their weights, and the losses of how the batch uses the experts: one pass over the logits backward."""
+    """Each token's experts and their weights, and with `balance` the losses of how the batch uses the experts (else zeros): one pass over the logits backward."""
 
     @staticmethod
-    def forward(ctx, logits, top_k):
+    def forward(ctx, logits, top_k, balance):
         experts, weights = nv.moe_route(logits, top_k)
-        losses, counts, _ = nv.moe_balance(logits, experts)
+        losses, counts, _ = nv.moe_balance(logits, experts) if balance else (logits.new_zeros(2), None, None)
         ctx.save_for_backward(logits, experts, counts)
         ctx.mark_non_differentiable(experts)
         return weights, losses, experts
@@ -76,12 +76,12 @@ class Route(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dweights, dlosses, _):
         logits, experts, counts = ctx.saved_tensors
-        return nv.moe_route_bwd(logits, experts, dweights.contiguous(), counts=counts, dlosses=dlosses.contiguous()), None
+        return nv.moe_route_bwd(logits, experts, dweights.contiguous(), counts=counts, dlosses=None if counts is None else dlosses.contiguous()), None, None
 
 
 class Experts(torch.nn.Module):
     """SwiGLU experts: out[t] = sum over the token's top_k experts of weight * down(silu(gate(x)) * up(x)).  balance: the weight of the balance loss, which forward() leaves in
-    balance_loss."""
+    balance_loss (0: none, and nothing is computed for it)."""
 
     def __init__(self, experts: int, top_k: int, width: int, hidden: int, dtype=torch.bfloat16, device="cuda", balance: float = 0.0):
         super().__init__()
@@ -91,7 +91,7 @@ class Experts(torch.nn.Module):
         self.gate_up, self.down = make(2 * hidden, width), make(width, hidden)  # (gate over up: one gather, one product)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        weights, losses, experts = Route.apply(self.router(x.float()), self.top_k)
+        weights, losses, experts = Route.apply(self.router(x.float()), self.top_k, self.balance != 0)
         self.balance_loss = self.balance * losses[0]
         offsets, order, position = nv.moe_sort(experts, self.down.shape[0])
         g, u = ExpertsLinear.apply(x, self.gate_up, offsets, order, position, self.top_k).chunk(2, dim=1)

@@ -158,3 +158,23 @@ def test_example_uses_them():
     a, b = v.detach().double().requires_grad_(), weight.detach().double().requires_grad_()
     (a / (a.square().mean(1, keepdim=True) + 1e-5).sqrt() * b).backward(up.double())
     assert (v.grad - a.grad).norm() <= 100 * 2.0 ** -24 * a.grad.norm() and (weight.grad - b.grad).norm() <= 100 * 2.0 ** -24 * b.grad.norm()
+
+
+def test_example_without_a_balance_loss_pays_for_none(monkeypatch):
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    import experts_training as ex
+    torch.manual_seed(0)
+    layer = ex.Experts(8, 2, 64, 128)
+    x, up = torch.randn(40, 64, device="cuda", dtype=torch.bfloat16), torch.randn(40, 2, device="cuda")
+    logits = [torch.randn(40, 8, generator=torch.Generator().manual_seed(0)).cuda().requires_grad_() for _ in range(2)]
+    with monkeypatch.context() as m:
+        m.setattr(ex.nv, "moe_balance", lambda *a: pytest.fail("asked for the balance"))
+        y = layer(x)
+        (y.float().square().mean() + layer.balance_loss).backward()
+        assert torch.isfinite(y).all() and layer.balance_loss == 0 and all(p.grad.any() for p in layer.parameters())
+        without = ex.Route.apply(logits[0], 2, False)
+        (without[0] * up).sum().backward()
+    # the same choice, weights and gradient as with a balance that nothing comes back from
+    beside = ex.Route.apply(logits[1], 2, True)
+    (beside[0] * up).sum().backward()
+    assert torch.equal(without[0], beside[0]) and torch.equal(without[2], beside[2]) and not without[1].any() and torch.equal(logits[0].grad, logits[1].grad)
