@@ -1038,9 +1038,9 @@ def moe_route(logits: torch.Tensor, top_k: int, renormalize: bool = True) -> Moe
     """nvfp4_moe_route: logits [T, E] -> each token's top_k experts, ties to the lower one, never one at -inf, and their weights: softmax over the chosen, or
     (renormalize False) shares of the softmax over all."""
     device, (T, E, ld) = _device_of(logits), _matrix(logits, "logits")
-    k = top_k if top_k > 0 else 0
+    k = top_k if 0 < top_k <= E else 0  # (0: refused by the call, before anything of that size is asked for)
     experts, weights = torch.empty(T, k, dtype=_I32, device=device), torch.empty(T, k, dtype=torch.float32, device=device)
-    code = lib.nvfp4_moe_route(logits.data_ptr(), _dtype_tag(logits), T, E, ld, top_k, renormalize, experts.data_ptr(), weights.data_ptr(), _stream())
+    code = lib.nvfp4_moe_route(logits.data_ptr(), _dtype_tag(logits), T, E, ld, k, renormalize, experts.data_ptr(), weights.data_ptr(), _stream())
     if code:
         _check(code, "nvfp4_moe_route")
     return MoeRoute(experts, weights)
@@ -1191,6 +1191,7 @@ def gemm_w4_experts(x: torch.Tensor, w, offsets: torch.Tensor, fmt: Format = NVF
     if groups < 1 or EN % groups or ng not in (1, groups):
         raise ValueError(f"a packed weight: [{groups} experts * N, {K}], with one g or one an expert")
     N, R = EN // groups, T if order is None else order.numel()
+    top_k = top_k if 0 < top_k < 1 << 31 else 0  # (0: refused by the call, where it counts; an argument of 32 bits)
     out = torch.empty(R, N, dtype=out_dtype, device=device)
     code = lib.nvfp4_gemm_w4_experts(R, N, K, groups, p_offsets, _format_ref(fmt), x.data_ptr(), _dtype_tag(x), ldx, T, p_order, top_k, p_codes, p_scales, p_g, int(ng > 1),
                                      out.data_ptr(), _dtype_tag(out), N, _stream())

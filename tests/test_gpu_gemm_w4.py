@@ -263,3 +263,12 @@ def test_a_sum_of_nothing_is_zero_whatever_g_is(M, g):
         got = nv.gemm_w4(x, w, out_dtype=out)
         assert got.shape == (M, 6) and (got == 0).all()
         assert (nv.gemm_w4_experts(x, w, torch.tensor([0, M, M], dtype=torch.int32, device="cuda"), out_dtype=out) == 0).all()
+
+
+@pytest.mark.parametrize("top_k", [0, -1, 1 << 31, (1 << 32) + 1, -(1 << 32) + 1, (1 << 64) + 1])
+def test_rows_of_a_token_that_no_call_takes(top_k):
+    # also where 32 bits of the number would be a number that is allowed
+    w, x = packed(32, 256, nv.NVFP4), torch.randn(4, 256, device="cuda")
+    o = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    with pytest.raises(nv.Nvfp4Error):
+        nv.gemm_w4_experts(x, w, o, order=torch.arange(4, dtype=torch.int32, device="cuda"), top_k=top_k)

@@ -327,3 +327,10 @@ def test_gradient_of_padding_is_zero_whatever_comes_back(E, dtype, renormalize, 
                 assert (d[::3] == 0).all() and not torch.isfinite(d[1::3]).all()
                 d = nv.moe_route_bwd(l.cuda(), experts, dw, renormalize=renormalize)
                 assert (d[::3] == 0).all()
+
+
+@pytest.mark.parametrize("k", [1 << 31, (1 << 32) + 2, 1 << 40, (1 << 64) + 2])
+def test_more_experts_than_there_are(k):
+    # refused before anything of that size is asked for, also where 32 bits of the number would be a number that is allowed
+    with pytest.raises(nv.Nvfp4Error):
+        nv.moe_route(torch.randn(1, 8, device="cuda"), k)
