@@ -683,6 +683,11 @@ int nvfp4_host_quantize_streams(int64_t rows, int64_t cols, int64_t ld, int both
  * time (of 0), workgroups of an output tile (of 3), else 1; whether the output leaves by streaming stores.  Returns 1, or 0 for sizes that launch nothing or
  * are refused.  Not a promise: the rules follow measurements. */
 int nvfp4_host_fp8_gemm_kernel(int32_t call, int64_t M, int64_t N, int64_t K, int32_t groups, nvfp4_dtype out_dt, int32_t choice[5]);
+/* Which kernel serves a product with a packed 4-bit weight on the current device: nvfp4_gemm_w4 (groups 0) or nvfp4_gemm_w4_experts; x_aligned: bf16 rows
+ * begin on 16-byte boundaries (with an order: and x has less than 2^32 bytes).  choice: 0 waves that divide the contraction (few rows), 1 tiles whose rows of x
+ * go to the LDS directly, 2 through registers; rows and columns of a workgroup's outputs; its waves.  Returns 1, or 0 for sizes that launch nothing or
+ * are refused.  Not a promise: the rules follow measurements. */
+int nvfp4_host_gemm_w4_kernel(int64_t rows, int64_t N, int64_t K, int32_t groups, nvfp4_dtype x_dt, int x_aligned, int32_t choice[4]);
 /* array forms: n inputs -> n outputs (host pointers) */
 void nvfp4_host_e4m3_encode_n(const float *r, int64_t n, uint8_t *out);
 void nvfp4_host_round_rtn_n(const float *m, int64_t n, uint8_t *out);

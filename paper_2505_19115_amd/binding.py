@@ -203,6 +203,8 @@ def _load() -> C.CDLL:
     L.nvfp4_gemm_w4.restype = L.nvfp4_gemm_w4_experts.restype = ci
     L.nvfp4_gemm_w4.argtypes = [i64, i64, i64, fp, vp, ci, i64, vp, vp, vp, vp, ci, i64, vp]
     L.nvfp4_gemm_w4_experts.argtypes = [i64, i64, i64, i32, vp, fp, vp, ci, i64, i64, vp, i32, vp, vp, vp, i32, vp, ci, i64, vp]
+    L.nvfp4_host_gemm_w4_kernel.restype = ci
+    L.nvfp4_host_gemm_w4_kernel.argtypes = [i64, i64, i64, i32, ci, ci, vp]
     L.nvfp4_probe_mfma_rate.restype = C.c_int
     L.nvfp4_probe_mfma_rate.argtypes = [C.c_int, C.c_int, C.c_int, vp, C.c_size_t, C.POINTER(C.c_double), vp]
     return L
@@ -242,7 +244,7 @@ EXPORTS = (
     "nvfp4_fp8_gemm_experts_dw", "nvfp4_moe_sort_workspace_bytes", "nvfp4_moe_sort", "nvfp4_moe_gather", "nvfp4_moe_combine", "nvfp4_moe_combine_bwd",
     "nvfp4_moe_combine_to", "nvfp4_moe_combine_to_bwd", "nvfp4_host_fp8_gemm_kernel",
     "nvfp4_moe_route", "nvfp4_moe_route_bwd", "nvfp4_moe_balance_workspace_bytes", "nvfp4_moe_balance", "nvfp4_layer_norm", "nvfp4_layer_norm_bwd_workspace_bytes",
-    "nvfp4_layer_norm_bwd", "nvfp4_gemm_w4", "nvfp4_gemm_w4_experts",
+    "nvfp4_layer_norm_bwd", "nvfp4_gemm_w4", "nvfp4_gemm_w4_experts", "nvfp4_host_gemm_w4_kernel",
 )
 
 
@@ -1198,3 +1200,20 @@ def gemm_w4_experts(x: torch.Tensor, w, offsets: torch.Tensor, fmt: Format = NVF
     if code:
         _check(code, "nvfp4_gemm_w4_experts")
     return out
+
+
+class W4Kernel(NamedTuple):
+    """What serves a product with a packed 4-bit weight: "few rows" (waves that divide the contraction), or tiles whose rows of x go to the LDS "direct" or "staged" through registers;
+    rows and columns of a workgroup's outputs; its waves."""
+    kernel: str
+    rows: int
+    cols: int
+    waves: int
+
+
+def gemm_w4_kernel(M: int, N: int, K: int, groups: int = 0, dtype: torch.dtype = torch.bfloat16, aligned: bool = True) -> W4Kernel | None:
+    """nvfp4_host_gemm_w4_kernel of gemm_w4 (groups 0) or gemm_w4_experts (M rows) for x of a type, its rows on 16-byte boundaries or not.  None: no kernel."""
+    choice = (C.c_int32 * 4)()
+    if not lib.nvfp4_host_gemm_w4_kernel(M, N, K, groups, F32 if dtype is torch.float32 else BF16, aligned, choice):
+        return None
+    return W4Kernel(("few rows", "direct", "staged")[choice[0]], choice[1], choice[2], choice[3])

@@ -126,6 +126,12 @@ nvfp4_status nvfp4_layer_norm_bwd(const void *dy, int64_t ldy, const void *x, in
     return done(launch_layer_norm_bwd(P, dt, dy, ldy, x, mean, rstd, dx, dweight, dbias, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
+static bool w4_sizes(int64_t rows, int64_t N, int64_t K, int32_t groups)
+{
+    return rows >= 0 && rows <= MOST_ROWS && N >= 0 && N <= MOST_ROWS && (groups <= 0 || groups * N <= MOST_ROWS) && K >= 0 && K <= MOST_WIDTH && K % 32 == 0 &&
+           (rows / 16 + groups + 2) * (N / 16 + 1) <= MOST_GRID;
+}
+
 static nvfp4_status product_w4(int64_t rows, int64_t N, int64_t K, int32_t groups, const int32_t *offsets, const nvfp4_format *f, const void *x, int x_dt, int64_t ldx,
                                int64_t x_rows, const int32_t *order, int32_t top_k, const uint8_t *codes, const uint8_t *scales, const float *g, int32_t g_step, void *out,
                                int out_dt, int64_t ldc, void *stream)
@@ -133,10 +139,7 @@ static nvfp4_status product_w4(int64_t rows, int64_t N, int64_t K, int32_t group
     if (!f || !valid_dtype(x_dt) || !valid_dtype(out_dt)) return NVFP4_EINVAL;
     if ((f->scale != NVFP4_SCALE_E4M3 && f->scale != NVFP4_SCALE_E8M0) || (f->tensor_scale != 0 && f->tensor_scale != 1)) return NVFP4_EINVAL;
     if (f->scale == NVFP4_SCALE_E8M0 ? f->block != 32 || f->tensor_scale : f->block != 16 && f->block != 32 && f->block != 64 && f->block != 128) return NVFP4_EUNSUPPORTED;
-    if (rows < 0 || rows > MOST_ROWS || N < 0 || N > MOST_ROWS || (groups > 0 && groups * N > MOST_ROWS) || K < 0 || K > MOST_WIDTH || K % 32 != 0 || K % f->block != 0 ||
-        ldx < K || ldc < N || x_rows < 0)
-        return NVFP4_ESHAPE;
-    if ((rows / 16 + groups + 2) * (N / 16 + 1) > MOST_GRID) return NVFP4_ESHAPE;
+    if (!w4_sizes(rows, N, K, groups) || K % f->block != 0 || ldx < K || ldc < N || x_rows < 0) return NVFP4_ESHAPE;
     if (!aligned(offsets, 4) || !aligned(order, 4)) return NVFP4_EALIGN;
     if (rows == 0 || N == 0) return NVFP4_OK;
     if (!out || (K > 0 && ((!x && x_rows > 0) || !codes || !scales)) || (f->tensor_scale && !g)) return NVFP4_EINVAL;
@@ -178,6 +181,25 @@ nvfp4_status nvfp4_gemm_w4_experts(int64_t rows, int64_t N, int64_t K, int32_t g
     if (groups < 1 || groups > MAX_EXPERTS || !offsets || (order && top_k < 1) || (W_scale_step != 0 && W_scale_step != 1)) return NVFP4_EINVAL;
     if (!order && x_rows < rows) return NVFP4_ESHAPE;
     return product_w4(rows, N, K, groups, offsets, f, x, raw(x_dt), ldx, x_rows, order, order ? top_k : 1, W_codes, W_scales, W_scale, W_scale_step, out, raw(out_dt), ldc, stream);
+}
+
+int nvfp4_host_gemm_w4_kernel(int64_t rows, int64_t N, int64_t K, int32_t groups, nvfp4_dtype x_dt, int x_aligned, int32_t choice[4])
+{
+    if (!choice || !valid_dtype(raw(x_dt)) || rows <= 0 || N <= 0 || groups < 0 || groups > MAX_EXPERTS || !w4_sizes(rows, N, K, groups)) return 0;
+    W4Args P = {};
+    P.x = reinterpret_cast<const uint8_t *>(x_aligned ? 16 : 18);  // (nobody follows it)
+    P.rows = P.x_rows = rows;
+    P.ldx = K;
+    P.N = P.ldc = N;
+    P.K = K;
+    P.groups = groups;
+    P.top_k = 1;
+    const W4Choice c = gemm_w4_choice(P, raw(x_dt));
+    choice[0] = c.kernel;
+    choice[1] = c.rows;
+    choice[2] = c.cols;
+    choice[3] = c.waves;
+    return 1;
 }
 
 }  // extern "C"

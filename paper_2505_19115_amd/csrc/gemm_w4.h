@@ -111,6 +111,8 @@ struct W4Tile {
     int rows16, cols16;
 };
 bool w4_takes_tiles(const W4Args &P, int x_dt, W4Tile *t);
+// Whether x goes to their LDS directly
+bool w4_takes_direct(const W4Args &P, int x_dt);
 hipError_t launch_gemm_w4_tiles(const W4Args &P, int x_dt, int out_dt, const W4Tile &t, hipStream_t st);
 
 }  // namespace nvfp4

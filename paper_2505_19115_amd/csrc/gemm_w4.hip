@@ -120,14 +120,22 @@ static hipError_t divided(W4Args P, int64_t slots, int out_dt, hipStream_t st)
 }
 
 constexpr int64_t MANY = 512;  // workgroups that fill the CUs with four waves each
+static int64_t row_slots(const W4Args &P) { return P.groups > 0 ? P.rows / 16 + (P.rows < P.groups + 1 ? P.rows : P.groups + 1) : 1; }
+static bool four_waves(const W4Args &P) { return (P.N + 15) / 16 * row_slots(P) >= MANY; }
 template <int XDT, int SC>
 static hipError_t few_rows(const W4Args &P, int out_dt, hipStream_t st)
 {
-    const int64_t slots = P.groups > 0 ? P.rows / 16 + (P.rows < P.groups + 1 ? P.rows : P.groups + 1) : 1;
-    return (P.N + 15) / 16 * slots >= MANY ? divided<XDT, SC, 4>(P, slots, out_dt, st) : divided<XDT, SC, 8>(P, slots, out_dt, st);
+    return four_waves(P) ? divided<XDT, SC, 4>(P, row_slots(P), out_dt, st) : divided<XDT, SC, 8>(P, row_slots(P), out_dt, st);
 }
 
 }  // namespace w4
+
+W4Choice gemm_w4_choice(const W4Args &P, int x_dt)
+{
+    W4Tile t;
+    if (w4_takes_tiles(P, x_dt, &t)) return {w4_takes_direct(P, x_dt) ? W4Choice::DIRECT : W4Choice::STAGED, 16 * t.rows16, 64 * t.cols16, 4};
+    return {W4Choice::FEW_ROWS, 16, 16, w4::four_waves(P) ? 4 : 8};
+}
 
 hipError_t launch_gemm_w4(const W4Args &P, int x_dt, int out_dt, hipStream_t st)
 {

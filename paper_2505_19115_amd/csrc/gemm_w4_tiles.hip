@@ -300,17 +300,11 @@ static hipError_t by_tile(const W4Args &P, int out_dt, const W4Tile &t, hipStrea
     else return t.rows16 == 7 ? with(integral_constant<int, 7>{}, integral_constant<int, 3>{}) : t.rows16 == 4 ? with(four, one) : with(two, one);
 }
 
-static bool takes_direct(const W4Args &P, int x_dt, int rows16)
-{
-    const int64_t span = P.order ? P.x_rows : 16 * rows16;  // (with an order any row of x may be a tile's)
-    return x_dt == NVFP4_BF16 && reinterpret_cast<uintptr_t>(P.x) % 16 == 0 && P.ldx % 8 == 0 && P.ldx < ((int64_t)1 << 31) / (span > 0 ? span : 1);
-}
-
 template <int XDT, int SC>
 static hipError_t by_form(const W4Args &P, int out_dt, const W4Tile &t, hipStream_t st)
 {
     if constexpr (XDT == NVFP4_BF16) {
-        if (takes_direct(P, XDT, 8)) return P.groups > 0 ? by_tile<XDT, SC, true, true>(P, out_dt, t, st) : by_tile<XDT, SC, false, true>(P, out_dt, t, st);
+        if (w4_takes_direct(P, XDT)) return P.groups > 0 ? by_tile<XDT, SC, true, true>(P, out_dt, t, st) : by_tile<XDT, SC, false, true>(P, out_dt, t, st);
     }
     return P.groups > 0 ? by_tile<XDT, SC, true, false>(P, out_dt, t, st) : by_tile<XDT, SC, false, false>(P, out_dt, t, st);
 }
@@ -348,13 +342,19 @@ static W4Tile cheapest(const W4Args &P, const TileCost (&of)[N])
 
 }  // namespace w4
 
+bool w4_takes_direct(const W4Args &P, int x_dt)
+{
+    const int64_t span = P.order ? P.x_rows : 16 * 8;  // (rows of a tile; with an order any row of x may be one)
+    return x_dt == NVFP4_BF16 && reinterpret_cast<uintptr_t>(P.x) % 16 == 0 && P.ldx % 8 == 0 && P.ldx < ((int64_t)1 << 31) / (span > 0 ? span : 1);
+}
+
 // More rows than one fragment has, of experts on average.  us, the kernel for few rows / tiles: 16 x 4096 x 11008 19 / 55, 16 x 12288 x 4096 26 / 24, 33 x 4096 x 4096 (four fragments of rows) 21 / 20,
 // 64 x 12288 x 4096 45 / 28, binary32 16 x 4096 x 11008 35 / 135, 64 x 12288 x 4096 93 / 64.
 bool w4_takes_tiles(const W4Args &P, int x_dt, W4Tile *t)
 {
     using namespace w4;
     if ((P.groups > 0 ? P.rows / P.groups : P.rows) <= 16) return false;
-    *t = x_dt == NVFP4_F32 ? cheapest(P, F32_TILES) : takes_direct(P, x_dt, 8) ? cheapest(P, DIRECT_TILES) : cheapest(P, STAGED_TILES);
+    *t = x_dt == NVFP4_F32 ? cheapest(P, F32_TILES) : w4_takes_direct(P, x_dt) ? cheapest(P, DIRECT_TILES) : cheapest(P, STAGED_TILES);
     return true;
 }
 

@@ -51,6 +51,12 @@ struct W4Args {
     uint32_t slots;                 // tiles of rows (set by launch_gemm_w4())
 };
 hipError_t launch_gemm_w4(const W4Args &P, int x_dt, int out_dt, hipStream_t st);
+// Which kernel that is: for few rows, or tiles whose rows of x go to the LDS directly or through registers; rows and columns of a workgroup's outputs, waves that share them
+struct W4Choice {
+    enum Kernel { FEW_ROWS, DIRECT, STAGED } kernel;
+    int rows, cols, waves;
+};
+W4Choice gemm_w4_choice(const W4Args &P, int x_dt);
 
 namespace layer {
 

@@ -272,3 +272,19 @@ def test_rows_of_a_token_that_no_call_takes(top_k):
     o = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
     with pytest.raises(nv.Nvfp4Error):
         nv.gemm_w4_experts(x, w, o, order=torch.arange(4, dtype=torch.int32, device="cuda"), top_k=top_k)
+
+
+@pytest.mark.parametrize("M", [1, 17, 140])
+def test_e8m0_scales_to_both_ends(M):
+    # every byte that nvfp4_quantize writes (0 .. 252), and every code; x picks single weights.  Weights under 2^-126 may count as 0
+    N, K = 64, 2048
+    codes = torch.arange(N * K // 2, dtype=torch.int64).mul(167).add(31).remainder(256).to(torch.uint8).view(N, K // 2)
+    scales = (torch.arange(N * K // 32) % 253).to(torch.uint8).view(N, K // 32)
+    v = values(codes, scales, nv.MXFP4)
+    at = torch.randint(0, K, (M,), generator=torch.Generator().manual_seed(M))
+    x = torch.zeros(M, K)
+    x[torch.arange(M), at] = 1.0
+    for dtype in DTYPES:
+        got = nv.gemm_w4(x.to(dtype).cuda(), (codes.cuda(), scales.cuda(), None), nv.MXFP4, out_dtype=torch.float32).cpu().double()
+        want = v[:, at].t()
+        assert ((got == want) | ((want.abs() < 2.0 ** -126) & (got == 0))).all()

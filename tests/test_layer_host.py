@@ -160,3 +160,23 @@ def test_launches_count_their_threads_in_32_bits(tmp_path):
     subprocess.check_call([CLANG, "-std=c++17", "-O1", "-x", "hip", "--offload-host-only", "-I/opt/rocm/include", "-o", exe, os.path.join(ROOT, "tests", "launch_grid_main.cpp"), "-L/opt/rocm/lib", "-lamdhip64"])
     p = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert p.returncode == 0 and "grids ok" in p.stdout, p.stderr
+
+
+B, F = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("args, kernel", [
+    ((1, 4096, 11008), ("few rows", 16, 16, 8)), ((16, 12288, 4096), ("few rows", 16, 16, 4)), ((32, 4096, 2048, 8), ("few rows", 16, 16, 4)), ((16, 300, 416, 0, F), ("few rows", 16, 16, 8)),
+    ((128, 40, 416, 8), ("few rows", 16, 16, 8)), ((17, 40, 416), ("direct", 32, 64, 4)), ((135, 40, 416, 8), ("few rows", 16, 16, 8)), ((136, 40, 416, 8), ("direct", 32, 64, 4)),
+    ((9000, 50, 416), ("direct", 64, 64, 4)), ((1500, 2049, 416), ("direct", 128, 64, 4)), ((9000, 700, 416), ("direct", 128, 128, 4)), ((777, 12288, 4096), ("direct", 112, 192, 4)),
+    ((4096, 4096, 4096), ("direct", 128, 256, 4)), ((17, 40, 416, 0, B, False), ("staged", 32, 64, 4)), ((9000, 130, 416, 0, B, False), ("staged", 64, 64, 4)),
+    ((1500, 2049, 416, 0, B, False), ("staged", 128, 128, 4)), ((65, 50, 416, 0, F), ("staged", 32, 64, 4)), ((3001, 130, 416, 0, F), ("staged", 32, 128, 4)), ((2000, 6001, 416, 0, F), ("staged", 32, 256, 4))])
+def test_which_kernel_serves_a_packed_product(args, kernel):
+    # (256 compute units where there is no GPU to ask)
+    assert nv.gemm_w4_kernel(*args) == kernel
+
+
+def test_no_packed_product_kernel():
+    for args in ((0, 4, 128), (4, 0, 128), (4, 4, 100), (4, 4, -32), (1 << 31, 4, 128), (4, 4, (1 << 23) + 32), ((1 << 31) - 1, (1 << 31) - 1, 128), (4, 1 << 22, 128, 512), (4, 4, 128, -1), (4, 4, 128, 513)):
+        assert nv.gemm_w4_kernel(*args) is None
+    assert L.nvfp4_host_gemm_w4_kernel(4, 4, 128, 0, BF16, 1, None) == 0 and L.nvfp4_host_gemm_w4_kernel(4, 4, 128, 0, 3, 1, (C.c_int32 * 4)()) == 0
