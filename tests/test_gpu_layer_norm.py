@@ -262,3 +262,17 @@ def test_column_sums_of_long_rows_keep_infinities():
         assert v[5] == float("inf") and torch.isnan(v[6]) and v[16390] == -float("inf") and v[9] == v[10] == float("inf")
         v[[5, 6, 9, 10, 16390]] = R
         assert (v == R).all()
+
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R, D", [(1024, 2056), (1025, 1030), (1025, 1537), (1027, 2048), (1025, 2049), (1030, 3333), (1026, 4096), (1100, 4104), (4099, 40), (1031, 12000)])
+def test_forward_many_rows(R, D, dtype, center):
+    # the rows from which another number of threads takes one, for the widths where it does
+    x, w, b = inputs(R, D, dtype, torch.float32, seed=2)
+    got = nv.layer_norm(x.cuda(), w.cuda(), b.cuda(), center=center)
+    y, m, r, bound, M, rel = norm64(x, w, b, 1e-5, center)
+    assert ((got.y.cpu().double() - y).abs() <= bound + HALF[dtype] * y.abs() * (1 + 2 ** -7) + 2.0 ** -130).all()
+    if center:
+        assert ((got.mean.cpu().double() - m).abs() <= M + U * m.abs()).all()
+    assert ((got.rstd.cpu().double() / r - 1).abs() <= rel + U).all()
