@@ -376,7 +376,7 @@ namespace norm {
 
 // f(threads of a row, pieces of a thread) of the forward kernel; false for rows that no workgroup holds
 template <class F>
-static bool with_row(int64_t rows, int64_t pieces, F &&f)
+static bool with_row(int64_t pieces, F &&f)
 {
     auto at = [&](auto t, auto u) { f(t, u); return true; };
     using std::integral_constant;
@@ -386,8 +386,9 @@ static bool with_row(int64_t rows, int64_t pieces, F &&f)
     if (pieces <= 64) return at(integral_constant<int, 64>{}, integral_constant<int, 1>{});
     if (pieces <= 128) return at(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     if (pieces <= 256) return at(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    // (few rows: a thread's loads, one behind the other, are what they wait for.  us, 64 threads / 256: 16 x 4096 bf16 6.7 / 3.8)
-    if (pieces <= 512) return rows <= 1024 ? at(integral_constant<int, 256>{}, integral_constant<int, 2>{}) : at(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+    // (us, 64 threads of eight pieces / 256 of two: 128 x 4096 bf16 5.7 / 3.5, 1024 rows 6.6 / 4.8, 8192 rows 31.8 / 21.2, 32768 rows 193 / 96; 32768 x 2304 129 / 67; binary32 128 x 2048 4.4 / 3.2,
+    // 32768 rows 101 / 92: eight pieces take 170 registers and their loads go out one behind the other)
+    if (pieces <= 512) return at(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     if (pieces <= 1024) return at(integral_constant<int, 256>{}, integral_constant<int, 4>{});
     if (pieces <= 2048) return at(integral_constant<int, 256>{}, integral_constant<int, 8>{});
     if (pieces <= 4096) return at(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
@@ -426,7 +427,7 @@ template <int DT>
 static hipError_t forward(const NormArgs &P, const uint8_t *x, float eps, uint8_t *y, float *mean, float *rstd, hipStream_t st)
 {
     const uint8_t *const w = reinterpret_cast<const uint8_t *>(P.weight), *const b = reinterpret_cast<const uint8_t *>(P.bias);
-    const bool held = norm::with_row(P.rows, (P.cols + norm::per_piece(DT) - 1) / norm::per_piece(DT), [&](auto t, auto u) {
+    const bool held = norm::with_row((P.cols + norm::per_piece(DT) - 1) / norm::per_piece(DT), [&](auto t, auto u) {
         constexpr int T = decltype(t)::value, U = decltype(u)::value, NT = T < 256 ? 256 : T;
         layer_norm_kernel<DT, T, U><<<launch_grid((P.rows + NT / T - 1) / (NT / T)), NT, 0, st>>>(x, P.rows, (int)P.cols, P.ld, w, b, P.wdt, P.center, eps, y, mean, rstd);
     });

@@ -268,7 +268,7 @@ def test_column_sums_of_long_rows_keep_infinities():
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("R, D", [(1024, 2056), (1025, 1030), (1025, 1537), (1027, 2048), (1025, 2049), (1030, 3333), (1026, 4096), (1100, 4104), (4099, 40), (1031, 12000)])
 def test_forward_many_rows(R, D, dtype, center):
-    # the rows from which another number of threads takes one, for the widths where it does
+    # many rows, and some that leave the last workgroup half empty
     x, w, b = inputs(R, D, dtype, torch.float32, seed=2)
     got = nv.layer_norm(x.cuda(), w.cuda(), b.cuda(), center=center)
     y, m, r, bound, M, rel = norm64(x, w, b, 1e-5, center)
@@ -276,3 +276,12 @@ def test_forward_many_rows(R, D, dtype, center):
     if center:
         assert ((got.mean.cpu().double() - m).abs() <= M + U * m.abs()).all()
     assert ((got.rstd.cpu().double() / r - 1).abs() <= rel + U).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [96, 1030, 1537, 2048, 2049, 3333, 4096, 4104, 9000])
+def test_a_row_alone(D, dtype):
+    # how many rows there are does not change a row's result
+    x, w, b = (t.cuda() for t in inputs(1100, D, dtype, torch.float32, seed=4))
+    many, few = nv.layer_norm(x, w, b), nv.layer_norm(x[:5], w, b)
+    assert all(torch.equal(m[:5], f) for m, f in zip(many, few))
