@@ -233,12 +233,6 @@ __global__ __launch_bounds__(256) void moe_route_bwd_kernel(const uint8_t *logit
 
 namespace route {
 
-// What a workgroup of the balance leaves of its tokens: probabilities summed, lse^2 summed [groups + 1]; pairs, tokens [groups + 1]
-struct Part {
-    float *sums;
-    int32_t *counts;
-};
-
 // Both losses and the means from the sums over all tokens; s_sums, s_counts: [groups + 1] in the LDS, behind a barrier
 __device__ __forceinline__ void balance_end(const float *s_sums, const int *s_counts, int groups, int top_k, int threads, float *per_wave, float *losses, int32_t *counts, float *probs)
 {
@@ -267,7 +261,8 @@ __device__ __forceinline__ void balance_end(const float *s_sums, const int *s_co
 
 constexpr int BALANCE_NT = 512;
 
-// A workgroup's tokens first .. last - 1: probabilities summed by the lanes that hold the columns, then over the workgroup's rows in their order
+// A workgroup's tokens first .. last - 1: probabilities summed by the lanes that hold the columns, then over the workgroup's rows in their order.  What it leaves of them: probabilities
+// summed and lse^2 summed [groups + 1]; pairs and tokens [groups + 1].
 template <int DT, int G, typename ID>
 __global__ __launch_bounds__(BALANCE_NT) void moe_balance_kernel(const uint8_t *logits, int64_t tokens, int groups, int64_t ld, int top_k, const ID *experts, int64_t part,
                                                                  float *part_sums, int32_t *part_counts, float *losses, int32_t *counts, float *probs)

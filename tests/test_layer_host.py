@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2505_19115_amd import binding as nv
+from test_device_code import LLVM, code_object, unwaited_loads
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CLANG = "/opt/rocm/lib/llvm/bin/clang++"
@@ -180,3 +181,10 @@ def test_no_packed_product_kernel():
     for args in ((0, 4, 128), (4, 0, 128), (4, 4, 100), (4, 4, -32), (1 << 31, 4, 128), (4, 4, (1 << 23) + 32), ((1 << 31) - 1, (1 << 31) - 1, 128), (4, 1 << 22, 128, 512), (4, 4, 128, -1), (4, 4, 128, 513)):
         assert nv.gemm_w4_kernel(*args) is None
     assert L.nvfp4_host_gemm_w4_kernel(4, 4, 128, 0, BF16, 1, None) == 0 and L.nvfp4_host_gemm_w4_kernel(4, 4, 128, 0, 3, 1, (C.c_int32 * 4)()) == 0
+
+
+def test_direct_loads_of_packed_products_wait_for_their_address(tmp_path):
+    # (a tile's first row may come of a lane read, and the loads stand in inline assembly, whose waits the compiler does not make)
+    asm = subprocess.run([os.path.join(LLVM, "llvm-objdump"), "-d", code_object("gemm_w4_tiles", tmp_path)], capture_output=True, text=True, check=True).stdout
+    loads, unwaited = unwaited_loads(asm)
+    assert loads > 0 and not unwaited
