@@ -18,14 +18,14 @@ KERNELS = [
     (BF16, True, 65, 50, ("direct", 32, 64, 4)), (BF16, True, 9000, 50, ("direct", 64, 64, 4)), (BF16, True, 1500, 2049, ("direct", 128, 64, 4)), (BF16, True, 9000, 700, ("direct", 128, 128, 4)),
     (BF16, True, 9000, 1001, ("direct", 112, 192, 4)), (BF16, True, 9000, 3001, ("direct", 128, 256, 4)),
     (BF16, False, 65, 50, ("staged", 32, 64, 4)), (BF16, False, 9000, 130, ("staged", 64, 64, 4)), (BF16, False, 1500, 2049, ("staged", 128, 128, 4)),
-    (F32, True, 65, 50, ("staged", 32, 64, 4)), (F32, True, 3001, 130, ("staged", 32, 128, 4)), (F32, True, 2000, 6001, ("staged", 32, 256, 4)),
+    (F32, True, 65, 50, ("staged", 32, 64, 4)), (F32, True, 1280, 1921, ("staged", 32, 128, 4)), (F32, True, 2000, 6001, ("staged", 32, 256, 4)),
 ]
 EXPERTS = [
     (BF16, True, 90, 40, 130, ("few rows", 16, 16, 8)), (BF16, True, 257, 40, 130, ("few rows", 16, 16, 4)), (BF16, False, 257, 40, 130, ("few rows", 16, 16, 4)), (F32, True, 257, 40, 130, ("few rows", 16, 16, 4)),
     (BF16, True, 65, 3, 50, ("direct", 32, 64, 4)), (BF16, True, 9000, 3, 50, ("direct", 64, 64, 4)), (BF16, True, 1500, 3, 2049, ("direct", 128, 64, 4)), (BF16, True, 9000, 3, 700, ("direct", 128, 128, 4)),
     (BF16, True, 9000, 3, 1001, ("direct", 112, 192, 4)), (BF16, True, 9000, 3, 3001, ("direct", 128, 256, 4)),
     (BF16, False, 65, 3, 50, ("staged", 32, 64, 4)), (BF16, False, 9000, 3, 130, ("staged", 64, 64, 4)), (BF16, False, 3001, 8, 1001, ("staged", 128, 128, 4)),
-    (F32, True, 65, 3, 50, ("staged", 32, 64, 4)), (F32, True, 3001, 3, 130, ("staged", 32, 128, 4)), (F32, True, 2000, 3, 6001, ("staged", 32, 256, 4)),
+    (F32, True, 65, 3, 50, ("staged", 32, 64, 4)), (F32, True, 1280, 3, 1921, ("staged", 32, 128, 4)), (F32, True, 2000, 3, 6001, ("staged", 32, 256, 4)),
 ]
 
 

@@ -171,7 +171,8 @@ B, F = torch.bfloat16, torch.float32
     ((128, 40, 416, 8), ("few rows", 16, 16, 8)), ((17, 40, 416), ("direct", 32, 64, 4)), ((135, 40, 416, 8), ("few rows", 16, 16, 8)), ((136, 40, 416, 8), ("direct", 32, 64, 4)),
     ((9000, 50, 416), ("direct", 64, 64, 4)), ((1500, 2049, 416), ("direct", 128, 64, 4)), ((9000, 700, 416), ("direct", 128, 128, 4)), ((777, 12288, 4096), ("direct", 112, 192, 4)),
     ((4096, 4096, 4096), ("direct", 128, 256, 4)), ((17, 40, 416, 0, B, False), ("staged", 32, 64, 4)), ((9000, 130, 416, 0, B, False), ("staged", 64, 64, 4)),
-    ((1500, 2049, 416, 0, B, False), ("staged", 128, 128, 4)), ((65, 50, 416, 0, F), ("staged", 32, 64, 4)), ((3001, 130, 416, 0, F), ("staged", 32, 128, 4)), ((2000, 6001, 416, 0, F), ("staged", 32, 256, 4))])
+    ((1500, 2049, 416, 0, B, False), ("staged", 128, 128, 4)), ((65, 50, 416, 0, F), ("staged", 32, 64, 4)), ((1280, 1920, 2048, 0, F), ("staged", 32, 128, 4)), ((2000, 6001, 416, 0, F), ("staged", 32, 256, 4)),
+    ((777, 12288, 4096, 0, F), ("staged", 32, 256, 4)), ((300, 12288, 4096, 0, F), ("staged", 32, 256, 4)), ((64, 12288, 4096, 0, F), ("staged", 32, 64, 4))])
 def test_which_kernel_serves_a_packed_product(args, kernel):
     # (256 compute units where there is no GPU to ask)
     assert nv.gemm_w4_kernel(*args) == kernel
