@@ -11,9 +11,10 @@ namespace nvfp4 {
 
 // 16 rows of the output by 16 columns a workgroup; its NW waves take the K tiles in turn, the codes of BATCH of them requested at a time and x of the next one, and their sums are
 // added through the LDS in the waves' order.  us, from memory, NW 4 / 8: 1 x 4096 x 11008 NVFP4 16.3 / 12.9, MXFP4 15.2 / 11.2, 16 x 12288 x 4096 19.8 / 19.7, 4 x 11008 x 2048 8.2 / 9.0, 16 tokens x 2
-// of 8 experts 4096 x 2048 MXFP4 19.8 / 24.2, 1 x 2 6.8 / 7.1, 8 x 2 of 64 1024 x 1024 7.6 / 9.9: eight where there are few columns.  The floor of the first is 4.8 us: a wave takes 0.5 us and more
-// for a K tile, whatever there is to load (1 x 256 x 12288, 1.7 MB, 11.8).  Tried: twelve K tiles' codes at a time and x of four (12.3, experts 25), four waves on columns of their own instead
-// of parts of the contraction (experts 25).
+// of 8 experts 4096 x 2048 MXFP4 19.8 / 24.2, 1 x 2 6.8 / 7.1, 8 x 2 of 64 1024 x 1024 7.6 / 9.9: eight where there are few columns.  The floor of the first is 4.8 us.  What the rest goes to: a batch of codes is asked for
+// at the top of the loop and waited for at once, because x, asked for behind it, is needed first and loads come in their order; between two batches nothing is on its way.  K = 11008 is three such
+// waits for each of eight waves, and one more a K tile for x (1 x 256 x 12288, 1.7 MB, takes 11.7).  Tried: twelve K tiles' codes at a time and x of four (12.3, experts 25), four waves on columns
+// of their own instead of parts of the contraction (experts 25).
 template <int XDT, int SC, int NW, bool GROUPED>
 __global__ __launch_bounds__(64 * NW) void gemm_w4_kernel(W4Args P, int out_dt)
 {

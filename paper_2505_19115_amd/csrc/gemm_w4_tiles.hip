@@ -3,9 +3,9 @@
 // quarter of a K tile ahead of the products: nothing of W is in the LDS, and each code is expanded once a tile (16 vector instructions for 8 codes with E4M3 scales, 4 with E8M0).
 // x goes through the LDS, two stages of a K tile, where all waves read it, a fragment at a time, three ahead.  bf16 rows on 16-byte boundaries go there by direct global -> LDS
 // loads, other rows through registers, binary32 ones as three bf16 pieces.
-// What bounds it: 4096^3 NVFP4 123 us (1.1 PFLOP/s, MXFP4 110; the instruction alone reaches 1.96 with two waves a SIMD), of which the expansion is a sixth, the rest waits: for the K
+// What bounds it: 4096^3 NVFP4 125 us (1.1 PFLOP/s, MXFP4 112; the instruction alone reaches 1.96 with two waves a SIMD), of which the expansion is a sixth, the rest waits: for the K
 // tile's loads, which a tile alone on its CU waits 0.4 us for, and at its barrier.  Tried: 32 x 32 x 16 products on one wave a SIMD, W through the LDS two K tiles ahead, one barrier a K tile
-// behind its last read (777 x 12288 x 4096 104 us, 94 here; 4096^3 144).
+// behind its last read (777 x 12288 x 4096 104 us, 92 here; 4096^3 144).  Tiles of 128 x 256 take all 256 registers and spill 2 to 6 of them (NVFP4; wider blocks by expert).
 // LDS image of a stage: row after row of 256 bytes, sixteen pieces of 16; piece c of row r stands at c ^ place(r), which spreads the rows that a fragment's
 // read is served with together over the banks (kernels.h).
 #include "gemm_w4.h"
@@ -350,7 +350,8 @@ bool w4_takes_direct(const W4Args &P, int x_dt)
 }
 
 // More rows than one fragment has, of experts on average.  us, the kernel for few rows / tiles: 16 x 4096 x 11008 19 / 55, 16 x 12288 x 4096 26 / 24, 33 x 4096 x 4096 (four fragments of rows) 21 / 20,
-// 64 x 12288 x 4096 45 / 28, binary32 16 x 4096 x 11008 35 / 135, 64 x 12288 x 4096 93 / 64.
+// 64 x 12288 x 4096 45 / 28, binary32 16 x 4096 x 11008 35 / 135, 64 x 12288 x 4096 93 / 59.  (Few columns and a long contraction lose by it: 17 x 4096 x 11008 58 where 16 rows take 18,
+// since nothing divides a tile's contraction.)
 bool w4_takes_tiles(const W4Args &P, int x_dt, W4Tile *t)
 {
     using namespace w4;

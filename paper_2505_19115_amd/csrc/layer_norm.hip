@@ -4,8 +4,11 @@
 // What bounds both is memory.  T threads hold a row in registers, U pieces of 16 bytes each, so that x (and dy) are read once and deviations come
 // from the mean, not from a difference of sums.  In the backward pass a thread keeps its columns from row to row: the weight stays in registers, the
 // sums for dw and db too; they meet in the LDS at the end, each workgroup leaves one row of sums, and a second kernel adds these in order.
-// us: forward 2049 x 2785 binary32 10.3 (4.4 TB/s); backward 8192 x 4096 bf16 54 + 5 (3.7 TB/s and 16 MB of sums written and read), 65536 rows of 96 bf16 18 + 4 (2 TB/s: half of
-// the lanes' second pieces lie past the row's end).  Tried: the next row's loads before this row's work (8192 x 4096 56, 65536 x 96 30).
+// us, kernels alone, rows from memory: forward 2049 x 2785 binary32 11.7 (3.9 TB/s; 9.9 where the last cache has them), 8192 x 4096 bf16 25.8 (5.2); backward 8192 x 4096 bf16 71 + 5 (2.9 TB/s,
+// and 16 MB of sums written and read; 54 + 5 from the cache), 65536 rows of 96 bf16 21 + 4 (1.8 TB/s: half of the lanes' second pieces lie past the row's end).  What holds the bf16 gradient
+// back: load_run() unpacks a piece in the branch that loads it, so that the compiler waits for each 16 bytes of x and dy before it asks for the next, four times a row; and 134 registers
+// of 256 threads leave a CU one workgroup of eight waves.  (Of the binary32 forms the one of 1024 threads spills 3 registers of 128.)  Tried: the next row's loads before this row's work (8192 x 4096
+// 56, 65536 x 96 30 from the cache), with loads that wait for one another all the same.
 #include <type_traits>
 
 #include "layer_ops.h"

@@ -5,8 +5,9 @@
 //   bwd      of weights over the chosen: dl_e = w_e (dw_e - sum_i w_i dw_i);  over the row: p_e (dw_e - sum_i w_i dw_i), dw_e = 0 where e is not chosen;
 //            of the balance: dL0 (E / N) p_e (f_e - sum_i f_i p_i), f taken as constants;  of lse^2: dL1 (2 / N) lse p_e
 // G lanes hold a row, eight entries each, so that a row of up to 512 experts is in registers and read once.
-// us, kernels alone: route 16 x 8 2.8 (a launch), 32768 x 128 bf16 k 8 10.8: eight rounds of some 50 instructions, where its 8 MB take 1.6; bwd 32768 x 128 binary32 with both gradients
-// 16.2 (34 MB: 6.3 at a copy's rate; the rest exponentials and finding the choices' lanes); balance 32768 x 256 bf16 13.6 + 10 (17 MB: 3.2).
+// us, kernels alone, rows from memory / from the last cache: route 16 x 8 2.5 (a launch), 32768 x 128 bf16 k 8 11.1 / 10.5: eight rounds of some 50 instructions, where its 8 MB take 1.6; bwd
+// 32768 x 128 binary32 with both gradients 17.5 / 15.8 (34 MB: 6.3 at a copy's rate; the rest exponentials and the search of the choices' lanes, 64 compares a lane); balance 32768 x 256 bf16
+// 14.7 / 13.0 (17 MB: 3.2; a group of lanes asks for its next row when it is done with one) + 10 (one workgroup reads 526 KB of sums).
 #include <math.h>
 
 #include "layer_ops.h"
